@@ -310,6 +310,102 @@ int moe_place_replicas(int32_t E, const int32_t* loads, const int32_t* replicas,
                        const int32_t* gpu_slots, int32_t max_segments, int32_t* gpu_of,
                        double* gpu_load, int32_t* gpu_count, int32_t* n_warm, void* hip_stream);
 
+/*
+ * Training a gate.  The paper's predictors are copies of later layers' gates that are fine-tuned on stored hidden
+ * states (Section 4.1); the same calls train a router.  A step is
+ *   moe_route_ws with scores_out -> moe_gate_distill and / or moe_balance_loss + moe_route_backward
+ *   -> moe_gate_backward -> moe_clip_grads over the gradients of all gates -> the caller's optimizer.
+ * Common to the calls below:
+ *   scores      [T,E] fp32, the scores_out of moe_route.  A score of -inf is an expert that is switched off:
+ *               probability 0; a token with no expert left has probabilities 0 and gets no gradient.
+ *   token_mask  [T] bytes, 0 = a padded token, or NULL (all tokens count).  Padded tokens add nothing to any sum and
+ *               their gradients are 0; nothing else that belongs to them is used, whatever it holds.
+ *   accumulate  gradients are added to what the output holds (a padded token's is then left as it was); 0: written
+ *   T == 0      is valid: sums over tokens are written as 0 (or left, with accumulate)
+ *   workspace   16-byte aligned, contents ignored on entry and undefined on return; one buffer of
+ *               moe_train_workspace_bytes() serves all calls of a shape that follow each other on a stream.  Calls that
+ *               share a workspace must not overlap in time (replays of captured graphs are calls).
+ * Sums over tokens are deterministic.  shape->F is not used.
+ */
+int moe_train_workspace_bytes(const moe_shape_t* shape, size_t* out_bytes);
+
+/*
+ * Load balance (Section 3.1: a few experts carry most tokens).  With N tokens that count, p = softmax_E(scores):
+ *   counts[e]   = number of assignments (t,j) with topk_idx[t,j] == e          [E] int32
+ *   prob_sum[e] = sum_t p[t,e]                                                  [E] fp32
+ *   loss        = E sum_e (counts[e] / (k N)) (prob_sum[e] / N)                 [1] fp32
+ *               = E k sum_e counts[e] prob_sum[e] / (sum_e counts[e])^2
+ * 1 for even loads and probabilities, E / k where k experts take everything; 0 if no token counts.  Indices outside
+ * [0,E) are assigned to nobody (N in the second form is then what is left).  The gradient: moe_route_backward.
+ */
+int moe_balance_loss(const moe_shape_t* shape, const float* scores, const int32_t* topk_idx,
+                     const uint8_t* token_mask, int32_t* counts, float* prob_sum, float* loss,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The scores' gradient of  sum_{t,j} d_topk_w[t,j] topk_w[t,j] + balance_coef * loss,  topk_w as moe_route defines it
+ * (shape->renorm) for the experts topk_idx, loss as above with the counts held fixed:
+ *   renorm 0   g_e = sum of d_topk_w[t,j] over j with topk_idx[t,j] == e;  d_scores[t,e]  = p_e (g_e - sum_l p_l g_l)
+ *   renorm 1   d_scores[t,topk_idx[t,j]] = w_j (d_topk_w[t,j] - sum_l w_l d_topk_w[t,l]),  w = topk_w[t,:]
+ *   balance    b_e = balance_coef E k counts[e] / (sum counts)^2;          d_scores[t,e] += p_e (b_e - sum_l p_l b_l)
+ * d_topk_w [T,k] fp32 or NULL (no routing part; topk_idx may then be NULL); counts [E] int32 or NULL (no balance
+ * part), for example those of moe_balance_loss, or their sums over the GPUs of a job.  Not both NULL.  An expert that
+ * a token lists twice gets both parts; indices outside [0,E) get none.  d_scores [T,E] fp32; accumulate 0 or 1.
+ */
+int moe_route_backward(const moe_shape_t* shape, const float* scores, const int32_t* topk_idx,
+                       const float* d_topk_w, const int32_t* counts, float balance_coef,
+                       const uint8_t* token_mask, float* d_scores, int accumulate, void* hip_stream);
+
+/*
+ * How far a gate is from the gate it predicts (Section 4.1): with p = softmax_E(scores), q = softmax_E(target_scores),
+ *   loss          = 1/N sum_t sum_e q[t,e] log(q[t,e] / p[t,e])     [1] fp32; 0 if no token counts
+ *   d_scores[t,e] = coef / N (p[t,e] - q[t,e])                      [T,E] fp32, or NULL (loss only)
+ * An expert that is switched off in target_scores alone asks for p = 0; one that is switched off in scores alone
+ * makes the loss infinite.  accumulate 0 or 1.
+ */
+int moe_gate_distill(const moe_shape_t* shape, const float* scores, const float* target_scores,
+                     const uint8_t* token_mask, float coef, float* loss, float* d_scores, int accumulate,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Gradients of the gate product (A1: score[t,e] = sum_i x[t,i] w_gate[e,i] + gate_bias[e]):
+ *   d_w_gate[e,:]  = sum_t d_scores[t,e] x[t,:]          [E,d] fp32, whatever `dtype` is, or NULL
+ *   d_gate_bias[e] = sum_t d_scores[t,e]                 [E] fp32, or NULL
+ *   d_x[t,:]       = sum_e d_scores[t,e] w_gate[e,:]     [T,d] in `dtype`, or NULL; rounded once
+ * At least one of them.  x is used for d_w_gate only, w_gate for d_x only (else they may be NULL), the workspace for
+ * d_w_gate and d_gate_bias.  accumulate: 0, or a sum of MOE_ACCUMULATE_WEIGHTS (d_w_gate and d_gate_bias: micro-batches)
+ * and MOE_ACCUMULATE_X (d_x: next to what the experts' gradients left there).
+ */
+#define MOE_ACCUMULATE_WEIGHTS 1
+#define MOE_ACCUMULATE_X 2
+int moe_gate_backward(const moe_shape_t* shape, const void* x, const void* w_gate, const float* d_scores,
+                      const uint8_t* token_mask, float* d_w_gate, float* d_gate_bias, void* d_x, int accumulate,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Global gradient norm and clipping over a list of tensors (the gradients of all gates of a model, say):
+ *   norm = sqrt(sum over all elements of all tensors of g^2), in 64 bits, stored as fp32 [1]
+ *   out  = g * c, one product and one rounding;  c = max_norm / norm if norm > max_norm, else 1
+ * If norm is not finite (an infinity or NaN among the gradients) c is 1: the caller finds it in `norm` and skips the
+ * step.  `tensors` is a HOST array, read before the call returns.  Tensors are contiguous; data and out need no more
+ * than their elements' alignment; `out` may be `data` (in place; nothing is written then if c is 1), but must not
+ * overlap the tensors otherwise, and no two outputs may overlap.  `out` is not used by moe_grad_norm.  n == 0 and
+ * count == 0 are valid.  max_norm: not negative, infinity allowed.  At most 2^40 elements.  workspace: as above, at
+ * least moe_grad_workspace_bytes() for the same list; a launch takes 128 tensors.
+ */
+typedef struct {
+  const void* data; /* device: n elements                                           */
+  void* out;        /* device: n elements, of the same type                         */
+  int64_t n;
+  int32_t dtype;    /* moe_dtype_t                                                  */
+  int32_t reserved; /* 0                                                            */
+} moe_tensor_t;
+int moe_grad_workspace_bytes(int32_t count, const moe_tensor_t* tensors, size_t* out_bytes);
+int moe_grad_norm(int32_t count, const moe_tensor_t* tensors, float* norm, void* workspace,
+                  size_t workspace_bytes, void* hip_stream);
+int moe_clip_grads(int32_t count, const moe_tensor_t* tensors, float max_norm, float* norm,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, human-readable text for a status code. */
 const char* moe_strerror(int code);
 

@@ -22,15 +22,24 @@ EXPORTS = ("moe_workspace_bytes", "moe_route", "moe_route_ws", "moe_count_and_pe
            "moe_grouped_ffn_part", "moe_grouped_ffn_gather",
            "moe_grouped_ffn_gather_part", "moe_grouped_ffn_combine_k1", "moe_ffn_workspace_bytes", "moe_grouped_ffn_ws", "moe_combine", "moe_scale_replicas", "moe_replica_segments",
            "moe_place_replicas",
+           "moe_train_workspace_bytes", "moe_balance_loss", "moe_route_backward", "moe_gate_distill",
+           "moe_gate_backward", "moe_grad_workspace_bytes", "moe_grad_norm", "moe_clip_grads",
            "moe_strerror")
 MOE_MAX_EXTRA_REPLICAS = 65536
 MOE_STATIC_SCRATCH_BYTES = 1 << 20
+MOE_ACCUMULATE_WEIGHTS = 1
+MOE_ACCUMULATE_X = 2
 
 
 class MoeShape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("E", ctypes.c_int32),
                 ("k", ctypes.c_int32), ("F", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("renorm", ctypes.c_int32)]
+
+
+class MoeTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -75,6 +84,18 @@ def load():
                                          i32p, vp]
     lib.moe_place_replicas.argtypes = [ctypes.c_int32, i32p, i32p, ctypes.c_int32, i32p, i32p, i32p,
                                        ctypes.c_int32, i32p, vp, i32p, i32p, vp]
+    lib.moe_train_workspace_bytes.argtypes = [shp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.moe_balance_loss.argtypes = [shp, f32p, i32p, vp, i32p, f32p, f32p, vp, ctypes.c_size_t, vp]
+    lib.moe_route_backward.argtypes = [shp, f32p, i32p, f32p, i32p, ctypes.c_float, vp, f32p,
+                                       ctypes.c_int, vp]
+    lib.moe_gate_distill.argtypes = [shp, f32p, f32p, vp, ctypes.c_float, f32p, f32p, ctypes.c_int, vp,
+                                     ctypes.c_size_t, vp]
+    lib.moe_gate_backward.argtypes = [shp, vp, vp, f32p, vp, f32p, f32p, vp, ctypes.c_int, vp,
+                                      ctypes.c_size_t, vp]
+    tsp = ctypes.POINTER(MoeTensor)
+    lib.moe_grad_workspace_bytes.argtypes = [ctypes.c_int32, tsp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.moe_grad_norm.argtypes = [ctypes.c_int32, tsp, f32p, vp, ctypes.c_size_t, vp]
+    lib.moe_clip_grads.argtypes = [ctypes.c_int32, tsp, ctypes.c_float, f32p, vp, ctypes.c_size_t, vp]
     lib.moe_strerror.argtypes = [ctypes.c_int]
     lib.moe_strerror.restype = ctypes.c_char_p
     for name in EXPORTS[:-1]:
@@ -227,3 +248,141 @@ def moe_place_replicas(E, loads, replicas, n_gpus, prev_replicas, prev_gpu, gpu_
                                      _ptr(prev_replicas), _ptr(prev_gpu), _ptr(gpu_slots),
                                      int(max_segments), _ptr(gpu_of), _ptr(gpu_load),
                                      _ptr(gpu_count), _ptr(n_warm), _stream(stream)))
+
+
+# ---- training a gate.  Tensors given to these calls are checked here (type, size, contiguity, the current GPU), as a
+# ---- mask or a gradient of another size would be read out of range; plain device addresses (int) are taken as they are.
+_F32, _I32, _MASK, _BYTES = "f32", "i32", "mask", "bytes"
+_types = None
+
+
+def _tensor_types():
+    """The torch types of each kind of argument; the kinds MOE_F32 and MOE_BF16 are storage in a shape's dtype."""
+    global _types
+    if _types is None:
+        import torch
+        _types = {_F32: (torch.float32,), _I32: (torch.int32,), _MASK: (torch.bool, torch.uint8),
+                  _BYTES: (torch.uint8, torch.int8), MOE_F32: (torch.float32,), MOE_BF16: (torch.bfloat16,)}
+    return _types
+
+
+def _addresses(call, *operands):
+    """Device addresses of (name, tensor or address or None, kind, elements) operands, after their checks.  A buffer of
+    bytes may be larger than asked for."""
+    out, gpu = [], None
+    for name, t, kind, numel in operands:
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        if gpu is None and t.is_cuda:
+            import torch
+            gpu = torch.cuda.current_device()
+        types = _tensor_types()[kind]
+        have = t.numel()
+        if t.get_device() != gpu or t.dtype not in types or not t.is_contiguous() or \
+                (have < numel if kind is _BYTES else have != numel):
+            raise ValueError(f"{call}: {name} has to be a contiguous tensor of {numel} x {' or '.join(map(str, types))} "
+                             f"on the current GPU, not {list(t.shape)} of {t.dtype}, strides {list(t.stride())}, on {t.device}")
+        out.append(t.data_ptr())
+    return out
+
+
+def moe_train_workspace_bytes(shape: MoeShape) -> int:
+    out = ctypes.c_size_t(0)
+    _check("moe_train_workspace_bytes",
+           load().moe_train_workspace_bytes(ctypes.byref(shape), ctypes.byref(out)))
+    return int(out.value)
+
+
+def moe_balance_loss(shape, scores, topk_idx, token_mask, counts, prob_sum, loss, workspace,
+                     workspace_bytes, stream=None):
+    T, E, k, nb = shape.T, shape.E, shape.k, int(workspace_bytes)
+    a = _addresses("moe_balance_loss", ("scores", scores, _F32, T * E), ("topk_idx", topk_idx, _I32, T * k),
+                   ("token_mask", token_mask, _MASK, T), ("counts", counts, _I32, E),
+                   ("prob_sum", prob_sum, _F32, E), ("loss", loss, _F32, 1), ("workspace", workspace, _BYTES, nb))
+    _check("moe_balance_loss", load().moe_balance_loss(ctypes.byref(shape), *a, nb, _stream(stream)))
+
+
+def moe_route_backward(shape, scores, topk_idx, d_topk_w, counts, balance_coef, token_mask, d_scores,
+                       accumulate=0, stream=None):
+    T, E, k = shape.T, shape.E, shape.k
+    a = _addresses("moe_route_backward", ("scores", scores, _F32, T * E), ("topk_idx", topk_idx, _I32, T * k),
+                   ("d_topk_w", d_topk_w, _F32, T * k), ("counts", counts, _I32, E),
+                   ("token_mask", token_mask, _MASK, T), ("d_scores", d_scores, _F32, T * E))
+    _check("moe_route_backward",
+           load().moe_route_backward(ctypes.byref(shape), *a[:4], float(balance_coef), *a[4:], int(accumulate),
+                                     _stream(stream)))
+
+
+def moe_gate_distill(shape, scores, target_scores, token_mask, coef, loss, d_scores, accumulate,
+                     workspace, workspace_bytes, stream=None):
+    T, E, nb = shape.T, shape.E, int(workspace_bytes)
+    a = _addresses("moe_gate_distill", ("scores", scores, _F32, T * E), ("target_scores", target_scores, _F32, T * E),
+                   ("token_mask", token_mask, _MASK, T), ("loss", loss, _F32, 1), ("d_scores", d_scores, _F32, T * E),
+                   ("workspace", workspace, _BYTES, nb))
+    _check("moe_gate_distill",
+           load().moe_gate_distill(ctypes.byref(shape), *a[:3], float(coef), *a[3:5], int(accumulate), a[5], nb,
+                                   _stream(stream)))
+
+
+def moe_gate_backward(shape, x, w_gate, d_scores, token_mask, d_w_gate, d_gate_bias, d_x, accumulate,
+                      workspace, workspace_bytes, stream=None):
+    T, d, E, nb = shape.T, shape.d, shape.E, int(workspace_bytes)
+    a = _addresses("moe_gate_backward", ("x", x, shape.dtype, T * d), ("w_gate", w_gate, shape.dtype, E * d),
+                   ("d_scores", d_scores, _F32, T * E), ("token_mask", token_mask, _MASK, T),
+                   ("d_w_gate", d_w_gate, _F32, E * d), ("d_gate_bias", d_gate_bias, _F32, E),
+                   ("d_x", d_x, shape.dtype, T * d), ("workspace", workspace, _BYTES, nb))
+    _check("moe_gate_backward",
+           load().moe_gate_backward(ctypes.byref(shape), *a[:7], int(accumulate), a[7], nb, _stream(stream)))
+
+
+class GradList:
+    """The tensors of moe_grad_norm and moe_clip_grads, marshalled once: `grads` and, for clipping, their outputs
+    (`out=None`: in place).  fp32 and bf16 tensors may be mixed.  Keeps the tensors alive."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if len(self.out) != len(self.grads):
+            raise ValueError(f"GradList: {len(self.grads)} gradients and {len(self.out)} outputs")
+        self.array = (MoeTensor * max(1, len(self.grads)))()
+        spans = []
+        for i, (g, o) in enumerate(zip(self.grads, self.out)):
+            dtype = MOE_BF16 if g.dtype in _tensor_types()[MOE_BF16] else MOE_F32
+            data, out = _addresses("GradList", (f"gradient {i}", g, dtype, g.numel()), (f"output {i}", o, dtype, g.numel()))
+            self.array[i] = MoeTensor(data, out, g.numel(), dtype, 0)
+            nbytes = g.numel() * g.element_size()
+            if nbytes:
+                if data != out:
+                    spans.append((data, nbytes, False))
+                spans.append((out, nbytes, True))
+        # an output may overlap nothing but the gradient that it replaces
+        end = out_end = 0
+        for start, nbytes, written in sorted(spans):
+            if start < (end if written else out_end):
+                raise ValueError("GradList: an output overlaps another tensor")
+            end = max(end, start + nbytes)
+            if written:
+                out_end = max(out_end, start + nbytes)
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def moe_grad_workspace_bytes(grads: GradList) -> int:
+    out = ctypes.c_size_t(0)
+    _check("moe_grad_workspace_bytes",
+           load().moe_grad_workspace_bytes(len(grads), grads.array, ctypes.byref(out)))
+    return int(out.value)
+
+
+def moe_grad_norm(grads: GradList, norm, workspace, workspace_bytes, stream=None):
+    nb = int(workspace_bytes)
+    a = _addresses("moe_grad_norm", ("norm", norm, _F32, 1), ("workspace", workspace, _BYTES, nb))
+    _check("moe_grad_norm", load().moe_grad_norm(len(grads), grads.array, *a, nb, _stream(stream)))
+
+
+def moe_clip_grads(grads: GradList, max_norm, norm, workspace, workspace_bytes, stream=None):
+    nb = int(workspace_bytes)
+    a = _addresses("moe_clip_grads", ("norm", norm, _F32, 1), ("workspace", workspace, _BYTES, nb))
+    _check("moe_clip_grads", load().moe_clip_grads(len(grads), grads.array, float(max_norm), *a, nb, _stream(stream)))

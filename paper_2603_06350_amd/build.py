@@ -12,7 +12,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmoe_gfx950.so")
-SOURCES = ["route.hip", "dispatch.hip", "ffn.hip", "combine.hip", "scaler.hip", "status.hip"]
+SOURCES = ["route.hip", "dispatch.hip", "ffn.hip", "combine.hip", "scaler.hip", "status.hip",
+           "gate_loss.hip", "gate_backward.hip", "grads.hip"]
 
 
 def hipcc() -> str:

@@ -24,6 +24,11 @@ namespace moe {
 inline int elem_bytes(int dtype) { return dtype == MOE_F32 ? 4 : 2; }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Workspace of the calls that train a gate; moe_train_workspace_bytes is the larger of the two.
+size_t gate_loss_workspace_bytes(const moe_shape_t* shape);
+size_t gate_backward_workspace_bytes(const moe_shape_t* shape);
 
 // Checks everything that does not depend on a particular call's pointers.
 inline int check_shape(const moe_shape_t* s) {
