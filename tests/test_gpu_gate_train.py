@@ -327,7 +327,8 @@ def check_gate(T, d, E, dtype, mask, seed, accumulate=0, parts="wbx", stream=Non
         if accumulate & flag and part in parts:
             o.t.copy_(torch.from_numpy(rng.standard_normal(tuple(o.t.shape)).astype(np.float32)))
             old[i] = o.t.double().cpu().numpy()
-    B.moe_gate_backward(sh, layer.to_device(poison(x, mask, nan)), layer.to_device(w), dev(poison(ds, mask)), dev(mask),
+    B.moe_gate_backward(sh, layer.to_device(poison(x, mask, nan)) if "w" in parts else None,
+                        layer.to_device(w) if "x" in parts else None, dev(poison(ds, mask)), dev(mask),
                         dw.t if "w" in parts else None, db.t if "b" in parts else None, dx.t if "x" in parts else None,
                         accumulate, ws, nb, stream)
     x64, w64 = orc.to_f64(x), orc.to_f64(w)
