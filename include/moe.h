@@ -374,7 +374,8 @@ int moe_gate_distill(const moe_shape_t* shape, const float* scores, const float*
  *   d_x[t,:]       = sum_e d_scores[t,e] w_gate[e,:]     [T,d] in `dtype`, or NULL; rounded once
  * At least one of them.  x is used for d_w_gate only, w_gate for d_x only (else they may be NULL), the workspace for
  * d_w_gate and d_gate_bias.  accumulate: 0, or a sum of MOE_ACCUMULATE_WEIGHTS (d_w_gate and d_gate_bias: micro-batches)
- * and MOE_ACCUMULATE_X (d_x: next to what the experts' gradients left there).
+ * and MOE_ACCUMULATE_X (d_x: next to what the experts' gradients left there).  Rows of x of at most 32 MiB (else
+ * MOE_ERR_UNSUPPORTED).
  */
 #define MOE_ACCUMULATE_WEIGHTS 1
 #define MOE_ACCUMULATE_X 2

@@ -17,6 +17,8 @@
 
 namespace moe {
 
+constexpr int64_t GB_ROW_BYTES = int64_t(1) << 25;   // of x: 32 of them stay within the 2^31 bytes of a buffer descriptor
+
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 gb_bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float gb_f32x4;
 
@@ -44,18 +46,37 @@ template <bool BF16, int V> struct GbFrag {
   uint4 f[P][V];
 };
 
+// A step's rows are read and written through a buffer descriptor of exactly these rows: the place of a lane in them is 32
+// bits, and a lane that is past the last row, or has nothing to do, reads zeros and writes nothing.  No load or store is
+// behind a branch, so that the waits for one step's operands can leave the next one's on their way.
+constexpr uint32_t GB_NOWHERE = 0x80000000u;          // a place outside every descriptor (with a few rows added as well)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t gb_rows(const void* first, int rows, uint32_t pitch) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, static_cast<int>(static_cast<uint32_t>(max(rows, 0)) * pitch), 0x00020000);
+}
+__device__ __forceinline__ float gb_load_f32(__amdgpu_buffer_rsrc_t rows, uint32_t at) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rows, static_cast<int>(at), 0, 0));
+}
+typedef uint32_t gb_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t gb_u32x2 __attribute__((ext_vector_type(2)));
+
 // V consecutive elements of a row: 8 or 16 bytes.
 template <bool BF16, int V> struct GbRow {
   static constexpr int W = V * (BF16 ? 2 : 4) / 4;
   uint32_t w[W];
-  __device__ __forceinline__ void load(const char* p) {
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rows, uint32_t at) {
     if constexpr (W == 4) {
-      const uint4 v = *reinterpret_cast<const uint4*>(p);
-      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+      const auto v = __builtin_amdgcn_raw_buffer_load_b128(rows, static_cast<int>(at), 0, 0);
+      w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
     } else {
-      const uint2 v = *reinterpret_cast<const uint2*>(p);
-      w[0] = v.x, w[1] = v.y;
+      const auto v = __builtin_amdgcn_raw_buffer_load_b64(rows, static_cast<int>(at), 0, 0);
+      w[0] = v[0], w[1] = v[1];
     }
+  }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t rows, uint32_t at) const {
+    if constexpr (W == 4)
+      __builtin_amdgcn_raw_buffer_store_b128(gb_u32x4{w[0], w[1], w[2], w[3]}, rows, static_cast<int>(at), 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b64(gb_u32x2{w[0], w[1]}, rows, static_cast<int>(at), 0, 0);
   }
   __device__ __forceinline__ void keep(bool real) {
 #pragma unroll
@@ -86,36 +107,77 @@ template <bool BF16, int V> __device__ __forceinline__ void gb_transpose(const G
 // keep their own sums in registers and add them up in LDS at the end.  (Waves side by side over the columns would
 // share the pieces of d_scores, but leave eight times the sums to be written and read again: for 65536 tokens, d = 2048,
 // 64 experts half of what x itself has.)
-constexpr int GW_THREADS = 512;
-constexpr int GW_WAVES = GW_THREADS / MOE_WAVE;
+//
+// d_scores: of up to 32 experts a lane loads the values it needs (8 tokens of an expert) one by one; of 64 they come
+// 16 bytes at a time straight into LDS, as single loads would keep the address units longer than the HBM takes for x.
+constexpr int GW_WAVES = 8;
+constexpr int GW_THREADS = GW_WAVES * MOE_WAVE;
+constexpr int GW_STAGE = 32 * 64 * 4;                 // bytes of one step's d_scores in LDS: 32 tokens, 64 experts
+constexpr int GW_RED = GW_WAVES * 4 * MOE_WAVE * 16;  // bytes of the sums of the waves
+template <int MT> constexpr int GW_LDS = MT < 4 ? GW_RED : 2 * GW_WAVES * GW_STAGE;
 
-template <bool BF16, int MT, int V>
-__global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(const char* __restrict__ x, const float* __restrict__ d_scores,
-                                                                 const uint8_t* __restrict__ mask, int T, int d, int E, int tiles,
-                                                                 int splits, int per_split, int accumulate,
-                                                                 float* __restrict__ out_w, float* __restrict__ out_b) {
-  __shared__ gb_f32x4 red[GW_WAVES][4][MOE_WAVE];
-  __shared__ float red_b[GW_WAVES][16 * MT];
+// What a wave multiplies in one step: 32 tokens, lane 16 g + c the tokens 8 g + 0..7 of its columns and experts.
+template <bool BF16, int MT, int V> struct GwStep {
+  GbRow<BF16, V> x[8];
+  float ds[MT < 4 ? MT : 1][8];
+  uint32_t mask;         // of token t0 + (lane & 31)
+  int left;              // tokens from t0 to the end, 32 at most
+};
+
+struct GwArgs {
+  const char* x;
+  const float* d_scores;
+  const uint8_t* mask;
+  float* out_w;
+  float* out_b;
+  int T, d, E, tiles, splits, per_split, accumulate;
+};
+
+// Eight values of LDS, 256 bytes apart.  Written out, because in front of a read that it places itself the compiler waits
+// for every load into LDS, those for the next step as well.
+__device__ __forceinline__ void gb_read_column(uint32_t at, float (&v)[8]) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  f32x2 a, b, c, d;
+  asm volatile(
+      "ds_read2st64_b32 %0, %4 offset0:0 offset1:1\n\t"
+      "ds_read2st64_b32 %1, %4 offset0:2 offset1:3\n\t"
+      "ds_read2st64_b32 %2, %4 offset0:4 offset1:5\n\t"
+      "ds_read2st64_b32 %3, %4 offset0:6 offset1:7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
+      : "v"(at)
+      : "memory");
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+
+template <int N> __device__ __forceinline__ void gb_wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// WHOLE: E is a multiple of 4, so that rows of d_scores are whole 16-byte chunks (of use with MT = 4 only).
+template <bool BF16, int MT, int V, bool WHOLE>
+__device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char* lds, float (*red_b)[16 * MT]) {
   constexpr int B = BF16 ? 2 : 4;
-  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, c = lane & 15, g = lane >> 4;
-  // All column tiles of a token range on one XCD (blocks are dealt to the 8 XCDs in turn): its L2 then gets d_scores
-  // once, and whole rows of x.
-  const int chunk = blockIdx.y;
-  int split, tile;
+  constexpr bool STAGED = MT == 4;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
+  const int d = a.d, E = a.E, tiles = a.tiles, splits = a.splits;
+  // All column tiles and groups of experts of a token range on one XCD (blocks are dealt to the 8 XCDs in turn): its L2
+  // then gets d_scores once, and whole rows of x once.
+  const int chunks = (E + 16 * MT - 1) / (16 * MT);
+  int split, rest;
   if (splits % 8 == 0) {
-    tile = blockIdx.x / 8 % tiles;
-    split = blockIdx.x / 8 / tiles * 8 + blockIdx.x % 8;
+    rest = blockIdx.x / 8 % (tiles * chunks);
+    split = blockIdx.x / 8 / (tiles * chunks) * 8 + blockIdx.x % 8;
   } else {
-    tile = blockIdx.x % tiles;
-    split = blockIdx.x / tiles;
+    rest = blockIdx.x % (tiles * chunks);
+    split = blockIdx.x / (tiles * chunks);
   }
-  const int e0 = chunk * 16 * MT;
-  const int col = tile * 16 * V + V * c;
-  const int64_t begin = static_cast<int64_t>(split) * per_split;
-  const int64_t end = min(begin + per_split, static_cast<int64_t>(T));
-  const char* x_lane = x + static_cast<int64_t>(min(col, d - V)) * B;
-  const int64_t pitch = static_cast<int64_t>(d) * B;
-  const bool with_bias = out_b && tile == 0;
+  const int tile = rest / chunks, e0 = rest % chunks * 16 * MT;
+  // (token numbers in 32 unsigned bits: T < 2^31, and no number passes it by more than the blocks' steps)
+  const uint32_t begin = static_cast<uint32_t>(split) * a.per_split;
+  const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
+  const uint32_t pitch = static_cast<uint32_t>(d) * B, pitch_s = static_cast<uint32_t>(E) * 4;
+  // Columns past the last and experts that do not exist repeat the last ones'; their sums are not stored.
+  const uint32_t at_x = 8 * g * pitch + static_cast<uint32_t>(min(tile * 16 * V + V * c, d - V)) * B;
+  const bool with_w = a.out_w, with_bias = a.out_b && tile == 0;
 
   gb_f32x4 acc[MT][V];
   float bias[MT];
@@ -126,35 +188,68 @@ __global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(const char* __r
     for (int i = 0; i < V; ++i) acc[m][i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int64_t t0 = begin + 32 * wave; t0 < end; t0 += 32 * GW_WAVES) {
-    GbRow<BF16, V> r[8];
-    const int left = static_cast<int>(min(end - t0, static_cast<int64_t>(32)));     // 1 .. 32 tokens
-    // bit i: token t0 + i counts
-    const int at = lane & 31;
-    const uint32_t real = static_cast<uint32_t>(__ballot(at < left && (!mask || mask[t0 + min(at, left - 1)])));
-    if (out_w) {
+  // STAGED: a row of 64 experts is 16 chunks of 16 bytes; chunk q of row r lies at place q ^ 4 (r / 8), so that the four
+  // lane groups, which read rows 8 apart, read different banks.
+  using Step = GwStep<BF16, MT, V>;
+  constexpr int SLOADS = STAGED ? (WHOLE ? 8 : 32) : 8 * MT;
+  auto load = [&](Step& s, uint32_t t0, unsigned char* stage) {
+    s.left = min(static_cast<int>(end - t0), 32);
+    // a descriptor for every row that the lanes have in common: what differs between lanes stays the same
+    const char* x0 = a.x + static_cast<int64_t>(t0) * pitch;
+    const char* s0 = reinterpret_cast<const char*>(a.d_scores) + static_cast<int64_t>(t0) * pitch_s;
+    s.mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? s.left : 0, 1), lane & 31, 0, 0);
+    if constexpr (STAGED) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j].load(x_lane + (t0 + min(8 * g + j, left - 1)) * pitch);
+      for (int i = 0; i < SLOADS; ++i) {
+        if constexpr (WHOLE) {
+          const int e = min(e0 + 4 * (c ^ 4 * (i / 2)), E - 4);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(gb_rows(s0 + 4 * i * pitch_s, s.left - 4 * i, pitch_s),
+                                                   (__attribute__((address_space(3))) void*)(stage + i * 1024), 16,
+                                                   static_cast<int>(g * pitch_s + e * 4), 0, 0, 0);
+        } else {
+          const int e = min(e0 + (lane ^ 16 * (i / 8)), E - 1);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(gb_rows(s0 + i * pitch_s, s.left - i, pitch_s),
+                                                   (__attribute__((address_space(3))) void*)(stage + i * 256), 4,
+                                                   static_cast<int>(e * 4), 0, 0, 0);
+        }
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j].keep(false);
-    }
-    if (real != 0xFFFFFFFFu) {
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j].keep(real >> (8 * g + j) & 1);
+        for (int j = 0; j < 8; ++j)
+          s.ds[m][j] = gb_load_f32(gb_rows(s0 + j * pitch_s, s.left - j, pitch_s),
+                                   8 * g * pitch_s + static_cast<uint32_t>(min(e0 + 16 * m + c, E - 1)) * 4);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s.x[j].load(gb_rows(x0 + static_cast<int64_t>(j) * pitch, with_w ? s.left - j : 0, pitch), at_x);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](Step& s, uint32_t stage_at) {
+    // the loads of the step that follows were issued last: all but those have arrived
+    gb_wait_loads<SLOADS + 8 + 1>();
+    uint32_t real = 0xFFu;                           // bit j: token t0 + 8 g + j counts
+    const bool some = a.mask || s.left < 32;
+    if (some) {
+      real = static_cast<uint32_t>(__ballot((lane & 31) < s.left && (!a.mask || s.mask))) >> (8 * g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s.x[j].keep(real >> j & 1);
     }
     GbFrag<BF16, V> b;
-    gb_transpose<BF16, V>(r, b);
+    gb_transpose<BF16, V>(s.x, b);
+    asm volatile("" : "+v"(stage_at));               // addresses are made anew in every step, not kept in registers
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      // rows of experts that do not exist repeat the last one's; their sums are not stored
-      const float* p = d_scores + t0 * E + min(e0 + 16 * m + c, E - 1);
       float v[8];
+      if constexpr (STAGED) {
+        gb_read_column(stage_at ^ 64 * m, v);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = p[static_cast<int64_t>(min(8 * g + j, left - 1)) * E];
-      if (real != 0xFFFFFFFFu) {
+        for (int j = 0; j < 8; ++j) v[j] = s.ds[m][j];
+      }
+      if (some) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = real >> (8 * g + j) & 1 ? v[j] : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = real >> j & 1 ? v[j] : 0.f;
       }
       if (with_bias) {
 #pragma unroll
@@ -178,13 +273,37 @@ __global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(const char* __r
         acc[m][i] = gb_mfma(ah, b.f[0][i], s);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // the next step's operands are on their way while this one's are multiplied; behind the last step nothing is read
+  {
+    unsigned char* stage0 = lds + wave * 2 * GW_STAGE;
+    unsigned char* stage1 = stage0 + GW_STAGE;
+    // where this lane finds expert c of the first of its 8 tokens; expert 16 m + c: 64 m in bits 6 and 7, by the places of
+    // the chunks (stages start at multiples of 256)
+    const uint32_t at0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)stage0)) + 2048 * g + 64 * g + 4 * c;
+    Step s0, s1;
+    uint32_t t0 = begin + 32 * wave;
+    load(s0, t0, stage0);
+    while (t0 < end) {
+      load(s1, t0 + 32 * GW_WAVES, stage1);
+      multiply(s0, at0);
+      t0 += 32 * GW_WAVES;
+      if (t0 >= end) break;
+      load(s0, t0 + 32 * GW_WAVES, stage0);
+      multiply(s1, at0 + GW_STAGE);
+      t0 += 32 * GW_WAVES;
+    }
+    gb_wait_loads<0>();                              // LDS is free for the sums
   }
+  __syncthreads();
 
   // sums of the waves, 16 experts at a time: lane 16 g + c of a wave holds experts 4 g + 0..3 of the columns V c + i
   const int64_t n = static_cast<int64_t>(E) * d;
-  float* to = out_w + (splits > 1 ? split * n : 0);
-  const bool add = accumulate && splits == 1;
-  if (out_w) {
+  float* to = a.out_w + (splits > 1 ? split * n : 0);
+  const bool add = a.accumulate && splits == 1;
+  auto red = reinterpret_cast<gb_f32x4(*)[4][MOE_WAVE]>(lds);
+  if (with_w) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -219,15 +338,20 @@ __global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(const char* __r
       if (g == 0) red_b[wave][16 * m + c] = v;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * MT; i += GW_THREADS) {
-      const int e = e0 + i;
-      if (e < E) {
-        float v = add ? out_b[e] : 0.f;
-        for (int w = 0; w < GW_WAVES; ++w) v += red_b[w][i];
-        out_b[(splits > 1 ? static_cast<int64_t>(split) * E : 0) + e] = v;
-      }
+    const int e = e0 + threadIdx.x;
+    if (threadIdx.x < 16 * MT && e < E) {
+      float v = add ? a.out_b[e] : 0.f;
+      for (int w = 0; w < GW_WAVES; ++w) v += red_b[w][threadIdx.x];
+      a.out_b[(splits > 1 ? static_cast<int64_t>(split) * E : 0) + e] = v;
     }
   }
+}
+
+template <bool BF16, int MT, int V, bool WHOLE>
+__global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(GwArgs a) {
+  extern __shared__ __align__(256) unsigned char lds[];
+  __shared__ float red_b[GW_WAVES][16 * MT];
+  gate_weight_block<BF16, MT, V, WHOLE>(a, lds, red_b);
 }
 
 // out[i] (+)= the sum of the parts' elements i, in order; four consecutive ones per thread.
@@ -259,107 +383,131 @@ static_assert(GS_THREADS >= MOE_MAX_E, "one thread per expert");
 constexpr int GX_THREADS = 256;
 constexpr int GX_WAVES = GX_THREADS / MOE_WAVE;
 
-template <bool BF16, int KS, int V>
-__global__ __launch_bounds__(GX_THREADS) void gate_x_kernel(const char* __restrict__ w_gate, const float* __restrict__ d_scores,
-                                                            const uint8_t* __restrict__ mask, int T, int d, int E, int tiles,
-                                                            int per_split, int accumulate, char* __restrict__ d_x) {
+struct GxArgs {
+  const char* w_gate;
+  const float* d_scores;
+  const uint8_t* mask;
+  char* d_x;
+  int T, d, E, tiles, per_split, accumulate;
+};
+
+// WHOLE: E is a multiple of 4, so that rows of d_scores are whole 16-byte chunks.  ACC: d_x is added to.
+template <bool BF16, int KS, int V, bool WHOLE, bool ACC>
+__global__ __launch_bounds__(GX_THREADS) void gate_x_kernel(GxArgs a) {
   constexpr int B = BF16 ? 2 : 4;
-  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, c = lane & 15, g = lane >> 4;
-  const int tile = static_cast<int>(blockIdx.x % tiles) * GX_WAVES + wave;
-  const int col = tile * 16 * V + V * c;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
+  const int d = a.d, E = a.E;
+  const int tile = static_cast<int>(blockIdx.x % a.tiles) * GX_WAVES + wave;
   if (tile * 16 * V >= d) return;
-  const int64_t begin = static_cast<int64_t>(blockIdx.x / tiles) * per_split;
-  const int64_t end = min(begin + per_split, static_cast<int64_t>(T));
-  const int64_t pitch = static_cast<int64_t>(d) * B;
-  const char* w_lane = w_gate + static_cast<int64_t>(min(col, d - V)) * B;
-  GbFrag<BF16, V> w[KS];
+  const int col = tile * 16 * V + V * c;
+  const uint32_t begin = blockIdx.x / a.tiles * static_cast<uint32_t>(a.per_split);
+  const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
+  const uint32_t pitch = static_cast<uint32_t>(d) * B, pitch_s = static_cast<uint32_t>(E) * 4;
+  struct Step {
+    float v[KS][8];
+    uint32_t mask;
+    GbRow<BF16, V> old[ACC ? 4 : 1];
+  };
+  // lane 16 g + c: experts 32 k + 8 g + 0..7 of token t0 + c; then tokens t0 + 4 g + 0..3 of its V columns
+  const uint32_t at_out = col < d ? 4 * g * pitch + static_cast<uint32_t>(col) * B : GB_NOWHERE;
+  auto load = [&](Step& s, uint32_t t0) {
+    const int rows = min(static_cast<int>(end - t0), 16);
+    const auto sr = gb_rows(a.d_scores + static_cast<int64_t>(t0) * E, rows, pitch_s);
+    s.mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? rows : 0, 1), c, 0, 0);
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    GbRow<BF16, V> r[8];
+    for (int k = 0; k < KS; ++k) {
+      const int e = 32 * k + 8 * g;
+      const uint32_t at = c * pitch_s + e * 4;
+      if constexpr (WHOLE) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = 32 * s + 8 * g + j;
-      r[j].load(w_lane + min(e, E - 1) * pitch);
-      r[j].keep(e < E);
+        for (int h = 0; h < 2; ++h) {
+          const auto q = __builtin_amdgcn_raw_buffer_load_b128(sr, static_cast<int>(e + 4 * h < E ? at + 16 * h : GB_NOWHERE), 0, 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s.v[k][4 * h + j] = __uint_as_float(q[j]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s.v[k][j] = gb_load_f32(sr, e + j < E ? at + 4 * j : GB_NOWHERE);
+      }
     }
-    gb_transpose<BF16, V>(r, w[s]);
+    if constexpr (ACC) {
+      const auto old = gb_rows(a.d_x + static_cast<int64_t>(t0) * pitch, rows, pitch);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s.old[r].load(old, at_out + r * pitch);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  uint32_t t0 = begin;
+  Step s0, s1;
+  load(s0, t0);
+  GbFrag<BF16, V> w[KS];
+  {
+    const uint32_t at = 8 * g * pitch + static_cast<uint32_t>(min(col, d - V)) * B;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const auto rows = gb_rows(a.w_gate + static_cast<int64_t>(32 * k) * pitch, min(E - 32 * k, 32), pitch);
+      GbRow<BF16, V> r[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j].load(rows, at + j * pitch);      // zeros for experts that do not exist
+      gb_transpose<BF16, V>(r, w[k]);
+    }
   }
-  const bool whole = E % 4 == 0;                     // rows of d_scores start at multiples of 16 bytes
-  for (int64_t t0 = begin; t0 < end; t0 += 16) {
-    const int64_t t = min(t0 + c, end - 1);          // this lane's token of d_scores
-    const bool real = !mask || mask[t];
+  auto multiply = [&](const Step& s, uint32_t t0) {
+    const int rows = min(static_cast<int>(end - t0), 16);
+    const bool real = !a.mask || s.mask;
     gb_f32x4 acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int e = 32 * s + 8 * g;
-      const float* p = d_scores + t * E;
-      float v[8];
-      if (whole) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float4 q = e + 4 * h < E ? *reinterpret_cast<const float4*>(p + e + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
-          v[4 * h] = q.x, v[4 * h + 1] = q.y, v[4 * h + 2] = q.z, v[4 * h + 3] = q.w;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = e + j < E ? p[e + j] : 0.f;
-      }
+    for (int k = 0; k < KS; ++k) {
       uint32_t q[3][4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float a = real ? v[2 * u] : 0.f, b = real ? v[2 * u + 1] : 0.f;
-        gb_split(a, b, q[0][u], q[1][u], q[2][u]);
-      }
+      for (int u = 0; u < 4; ++u)
+        gb_split(real ? s.v[k][2 * u] : 0.f, real ? s.v[k][2 * u + 1] : 0.f, q[0][u], q[1][u], q[2][u]);
       const uint4 ah = make_uint4(q[0][0], q[0][1], q[0][2], q[0][3]), am = make_uint4(q[1][0], q[1][1], q[1][2], q[1][3]),
                   al = make_uint4(q[2][0], q[2][1], q[2][2], q[2][3]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         if constexpr (!BF16) {
-          acc[i] = gb_mfma(al, w[s].f[0][i], acc[i]);
-          acc[i] = gb_mfma(ah, w[s].f[2][i], acc[i]);
-          acc[i] = gb_mfma(am, w[s].f[1][i], acc[i]);
+          acc[i] = gb_mfma(al, w[k].f[0][i], acc[i]);
+          acc[i] = gb_mfma(ah, w[k].f[2][i], acc[i]);
+          acc[i] = gb_mfma(am, w[k].f[1][i], acc[i]);
         }
-        acc[i] = gb_mfma(am, w[s].f[0][i], acc[i]);
-        if constexpr (!BF16) acc[i] = gb_mfma(ah, w[s].f[1][i], acc[i]);
-        acc[i] = gb_mfma(ah, w[s].f[0][i], acc[i]);
+        acc[i] = gb_mfma(am, w[k].f[0][i], acc[i]);
+        if constexpr (!BF16) acc[i] = gb_mfma(ah, w[k].f[1][i], acc[i]);
+        acc[i] = gb_mfma(ah, w[k].f[0][i], acc[i]);
       }
     }
-    // lane 16 g + c holds tokens t0 + 4 g + 0..3 of its V columns
-    const uint64_t keep = __ballot(real);            // bit i of the first 16: token t0 + i counts
+    // padded tokens: zeros, or nothing where d_x is added to
+    const uint32_t keep = ACC ? static_cast<uint32_t>(__ballot(real)) : 0xFFFFu;       // bit i: token t0 + i counts
+    const auto out = gb_rows(a.d_x + static_cast<int64_t>(t0) * pitch, rows, pitch);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t to = t0 + 4 * g + r;
-      if (to >= end || col >= d || (accumulate && !(keep >> (4 * g + r) & 1))) continue;
-      char* o = d_x + to * pitch + static_cast<int64_t>(col) * B;
-      GbRow<BF16, V> old;
-      if (accumulate) old.load(o);
-      if constexpr (BF16) {
-        uint32_t q[V / 2];
+      GbRow<BF16, V> o;
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-          float a = acc[2 * i][r], b = acc[2 * i + 1][r];
-          if (accumulate) {
-            a += bf16lo(old.w[i]);
-            b += bf16hi(old.w[i]);
-          }
-          q[i] = pack_bf16x2(a, b);
+      for (int i = 0; i < o.W; ++i) {
+        if constexpr (BF16) {
+          float lo = acc[2 * i][r], hi = acc[2 * i + 1][r];
+          if constexpr (ACC) lo += bf16lo(s.old[r].w[i]), hi += bf16hi(s.old[r].w[i]);
+          o.w[i] = pack_bf16x2(lo, hi);
+        } else {
+          float v = acc[i][r];
+          if constexpr (ACC) v += __uint_as_float(s.old[r].w[i]);
+          o.w[i] = __float_as_uint(v);
         }
-        if constexpr (V == 8)
-          *reinterpret_cast<uint4*>(o) = make_uint4(q[0], q[1], q[2], q[3]);
-        else
-          *reinterpret_cast<uint2*>(o) = make_uint2(q[0], q[1]);
-      } else {
-        float q[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) q[i] = acc[i][r] + (accumulate ? __uint_as_float(old.w[i]) : 0.f);
-        if constexpr (V == 4)
-          *reinterpret_cast<float4*>(o) = make_float4(q[0], q[1], q[2], q[3]);
-        else
-          *reinterpret_cast<float2*>(o) = make_float2(q[0], q[1]);
       }
+      o.store(out, keep >> (4 * g + r) & 1 ? at_out + r * pitch : GB_NOWHERE);
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  while (t0 < end) {
+    load(s1, t0 + 16);
+    multiply(s0, t0);
+    t0 += 16;
+    if (t0 >= end) break;
+    load(s0, t0 + 16);
+    multiply(s1, t0);
+    t0 += 16;
   }
 }
 
@@ -371,12 +519,12 @@ struct GwPlan {
 };
 static GwPlan gw_plan(const moe_shape_t* s) {
   GwPlan p{};
-  p.mt = s->E <= 16 ? 1 : s->E <= 32 ? 2 : s->E <= 64 ? 4 : 8;
-  p.v = s->dtype == MOE_F32 || p.mt == 8 ? 4 : 8;
+  p.mt = s->E <= 16 ? 1 : s->E <= 32 ? 2 : 4;
+  p.v = s->dtype == MOE_F32 ? 4 : 8;
   p.tiles = (s->d + 16 * p.v - 1) / (16 * p.v);
   p.chunks = (s->E + 16 * p.mt - 1) / (16 * p.mt);
   const int64_t most = (static_cast<int64_t>(s->T) + 32 * GW_WAVES - 1) / (32 * GW_WAVES);
-  int64_t n = 512 / (static_cast<int64_t>(p.tiles) * p.chunks);
+  int64_t n = (p.mt == 4 ? 256 : 512) / (static_cast<int64_t>(p.tiles) * p.chunks);
   if (n > most) n = most;
   if (n > 8) n = n / 8 * 8;
   if (n < 1) n = 1;
@@ -392,33 +540,45 @@ size_t gate_backward_workspace_bytes(const moe_shape_t* shape) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * shape->E * (static_cast<size_t>(shape->d) + 1) * sizeof(float) : 0;
 }
 
-template <bool BF16>
-static void launch_weight(const GwPlan& p, const moe_shape_t* s, const void* x, const float* ds, const uint8_t* mask, int accumulate,
-                          float* out_w, float* out_b, hipStream_t st) {
-  constexpr int V8 = BF16 ? 8 : 4;
-  const auto kernel = p.mt == 1 ? gate_weight_kernel<BF16, 1, V8> : p.mt == 2 ? gate_weight_kernel<BF16, 2, V8>
-                    : p.mt == 4 ? gate_weight_kernel<BF16, 4, V8> : gate_weight_kernel<BF16, 8, 4>;
-  hipLaunchKernelGGL(kernel, dim3(p.tiles * p.splits, p.chunks), dim3(GW_THREADS), 0, st, static_cast<const char*>(x), ds, mask, s->T,
-                     s->d, s->E, p.tiles, p.splits, p.per_split, accumulate, out_w, out_b);
+template <bool BF16, int MT, bool WHOLE> static int launch_weight(const GwPlan& p, const GwArgs& a, hipStream_t st) {
+  constexpr int V = BF16 ? 8 : 4;
+  const auto kernel = gate_weight_kernel<BF16, MT, V, WHOLE>;
+  static LdsOnce once;
+  const int rc = ensure_dynamic_lds(once, reinterpret_cast<const void*>(kernel), GW_LDS<MT>);
+  if (rc != MOE_OK) return rc;
+  hipLaunchKernelGGL(kernel, dim3(p.tiles * p.chunks * p.splits), dim3(GW_THREADS), GW_LDS<MT>, st, a);
+  return MOE_OK;
+}
+
+template <bool BF16, int KS, int V> static void launch_x(const GxArgs& a, dim3 grid, hipStream_t st) {
+  const bool whole = a.E % 4 == 0;
+  const auto kernel = a.accumulate ? (whole ? gate_x_kernel<BF16, KS, V, true, true> : gate_x_kernel<BF16, KS, V, false, true>)
+                                   : (whole ? gate_x_kernel<BF16, KS, V, true, false> : gate_x_kernel<BF16, KS, V, false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(GX_THREADS), 0, st, a);
 }
 
 template <bool BF16>
-static void launch_x(const moe_shape_t* s, const void* w, const float* ds, const uint8_t* mask, int accumulate, void* d_x, hipStream_t st) {
+static void x_grad(const moe_shape_t* s, const void* w, const float* ds, const uint8_t* mask, int accumulate, void* d_x, hipStream_t st) {
   constexpr int V8 = BF16 ? 8 : 4, V4 = BF16 ? 4 : 2;
-  const int ks = s->E <= 32 ? 1 : s->E <= 64 ? 2 : s->E <= 128 ? 4 : 8;
-  const int v = ks <= 2 ? V8 : V4;
-  const auto kernel = ks == 1 ? gate_x_kernel<BF16, 1, V8> : ks == 2 ? gate_x_kernel<BF16, 2, V8>
-                    : ks == 4 ? gate_x_kernel<BF16, 4, V4> : gate_x_kernel<BF16, 8, V4>;
+  const int v = s->E <= 64 ? V8 : V4;
   const int tiles = (s->d + 16 * v * GX_WAVES - 1) / (16 * v * GX_WAVES);
-  int64_t splits = 2048 / tiles;
+  int64_t splits = 1024 / tiles;
   const int64_t most = (static_cast<int64_t>(s->T) + 15) / 16;
   if (splits > most) splits = most;
   if (splits < 1) splits = 1;
   int64_t per = (s->T + splits - 1) / splits;
   per = (per + 15) / 16 * 16;
   splits = (s->T + per - 1) / per;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tiles * splits)), dim3(GX_THREADS), 0, st, static_cast<const char*>(w), ds, mask,
-                     s->T, s->d, s->E, tiles, static_cast<int>(per), accumulate, static_cast<char*>(d_x));
+  const GxArgs a = {static_cast<const char*>(w), ds, mask, static_cast<char*>(d_x), s->T, s->d, s->E, tiles, static_cast<int>(per), accumulate};
+  const dim3 grid(static_cast<unsigned>(tiles * splits));
+  if (s->E <= 32)
+    launch_x<BF16, 1, V8>(a, grid, st);
+  else if (s->E <= 64)
+    launch_x<BF16, 2, V8>(a, grid, st);
+  else if (s->E <= 128)
+    launch_x<BF16, 4, V4>(a, grid, st);
+  else
+    launch_x<BF16, 8, V4>(a, grid, st);
 }
 
 template <bool BF16>
@@ -430,15 +590,18 @@ static int gate_backward(const moe_shape_t* shape, const void* x, const void* w_
     const int64_t n = static_cast<int64_t>(shape->E) * shape->d;
     const bool parts = p.splits > 1;
     float* part_b = part + p.splits * n;
-    launch_weight<BF16>(p, shape, x, d_scores, mask, acc_w, d_w_gate ? (parts ? part : d_w_gate) : nullptr,
-                        d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, st);
+    const GwArgs a = {static_cast<const char*>(x), d_scores, mask, d_w_gate ? (parts ? part : d_w_gate) : nullptr,
+                      d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, shape->T, shape->d, shape->E, p.tiles, p.splits, p.per_split, acc_w};
+    const int rc = p.mt == 1 ? launch_weight<BF16, 1, true>(p, a, st) : p.mt == 2 ? launch_weight<BF16, 2, true>(p, a, st)
+                 : shape->E % 4 == 0 ? launch_weight<BF16, 4, true>(p, a, st) : launch_weight<BF16, 4, false>(p, a, st);
+    if (rc != MOE_OK) return rc;
     if (parts) {
       const int64_t threads = d_w_gate ? n / 4 : 1;
       hipLaunchKernelGGL(gate_sum_kernel, dim3(static_cast<unsigned>((threads + GS_THREADS - 1) / GS_THREADS)), dim3(GS_THREADS), 0, st, part,
                          d_w_gate, n, part_b, d_gate_bias, shape->E, p.splits, acc_w);
     }
   }
-  if (d_x && shape->T > 0) launch_x<BF16>(shape, w_gate, d_scores, mask, acc_x, d_x, st);
+  if (d_x && shape->T > 0) x_grad<BF16>(shape, w_gate, d_scores, mask, acc_x, d_x, st);
   return launch_status();
 }
 
@@ -464,6 +627,7 @@ extern "C" int moe_gate_backward(const moe_shape_t* shape, const void* x, const 
   if (!d_w_gate && !d_gate_bias && !d_x) return shape->T == 0 ? MOE_OK : MOE_ERR_INVALID_ARG;
   if (!aligned16(d_w_gate) || !aligned4(d_gate_bias) || !aligned16(d_x) || !aligned16(x) || !aligned16(w_gate) || !aligned16(d_scores))
     return MOE_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(shape->d) * elem_bytes(shape->dtype) > GB_ROW_BYTES) return MOE_ERR_UNSUPPORTED;
   if (shape->T > 0 && (!d_scores || (d_w_gate && !x) || (d_x && !w_gate))) return MOE_ERR_INVALID_ARG;
   if (d_w_gate || d_gate_bias) {
     if (!workspace || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
