@@ -102,6 +102,22 @@ template <bool BF16, int V> __device__ __forceinline__ void gb_transpose(const G
   }
 }
 
+// acc[i] += the products of the pieces of an fp32 operand (TWO: without the last) with those of column tile i, the small
+// ones first.  Products with the same sum are V instructions apart: one that follows directly waits for the sum.
+template <bool BF16, bool TWO, int V>
+__device__ __forceinline__ void gb_products(uint4 h, uint4 m, uint4 l, const GbFrag<BF16, V>& b, gb_f32x4 (&acc)[V]) {
+  auto step = [&](uint4 a, const uint4 (&f)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = gb_mfma(a, f[i], acc[i]);
+  };
+  if constexpr (!TWO) step(l, b.f[0]);
+  if constexpr (!BF16) step(h, b.f[2]);
+  if constexpr (!BF16) step(m, b.f[1]);
+  step(m, b.f[0]);
+  if constexpr (!BF16) step(h, b.f[1]);
+  step(h, b.f[0]);
+}
+
 // ------------------------------------------------------------------------------------------------ weights' gradient
 // A block owns 16 V columns of x for a range of tokens and up to 16 MT experts; its waves take 32 tokens each in turn,
 // keep their own sums in registers and add them up in LDS at the end.  (Waves side by side over the columns would
@@ -260,18 +276,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char
       for (int u = 0; u < 4; ++u) gb_split(v[2 * u], v[2 * u + 1], q[0][u], q[1][u], q[2][u]);
       const uint4 ah = make_uint4(q[0][0], q[0][1], q[0][2], q[0][3]), am = make_uint4(q[1][0], q[1][1], q[1][2], q[1][3]),
                   al = make_uint4(q[2][0], q[2][1], q[2][2], q[2][3]);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        gb_f32x4 s = acc[m][i];
-        s = gb_mfma(al, b.f[0][i], s);
-        if constexpr (!BF16) {
-          s = gb_mfma(ah, b.f[2][i], s);
-          s = gb_mfma(am, b.f[1][i], s);
-        }
-        s = gb_mfma(am, b.f[0][i], s);
-        if constexpr (!BF16) s = gb_mfma(ah, b.f[1][i], s);
-        acc[m][i] = gb_mfma(ah, b.f[0][i], s);
-      }
+      gb_products<BF16, false, V>(ah, am, al, b, acc[m]);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -378,8 +383,10 @@ __global__ __launch_bounds__(GS_THREADS) void gate_sum_kernel(const float* __res
 static_assert(GS_THREADS >= MOE_MAX_E, "one thread per expert");
 
 // ------------------------------------------------------------------------------------------------ hidden states' gradient
-// A wave keeps the fragments of w_gate of its 16 V columns (KS steps of 32 experts) in registers and runs over tokens,
-// 16 at a time: d_scores in, d_x out.  The four waves of a block lie side by side.
+// A wave keeps the fragments of w_gate of its 16 V columns (KS steps of 32 experts) in registers; the four waves of a
+// block lie side by side and run over tokens, GT at a time.  The block reads d_scores of its next GT tokens in whole
+// rows, cuts them into pieces once and keeps these in LDS, from where the waves take their operands.  (Every wave
+// reading its operands straight from global memory: 64 lanes in 64 places, which the L1 serves one after the other; XXX.)
 constexpr int GX_THREADS = 256;
 constexpr int GX_WAVES = GX_THREADS / MOE_WAVE;
 
@@ -388,58 +395,77 @@ struct GxArgs {
   const float* d_scores;
   const uint8_t* mask;
   char* d_x;
-  int T, d, E, tiles, per_split, accumulate;
+  int T, d, E, tiles, splits, per_split;
+};
+
+template <bool BF16, int KS> struct GxTile {
+  static constexpr int P = BF16 ? 2 : 3;             // pieces of d_scores
+  static constexpr int GT = KS <= 2 ? 64 : 128 / KS; // tokens of a step
+  static constexpr int CPT = 8 * KS;                 // chunks of four experts of a token
+  static constexpr int LOADS = GT * CPT / GX_THREADS;
+  static constexpr int PITCH = 64 * KS + 16;         // bytes of a row in LDS: 16 more than the experts take, against bank conflicts
 };
 
 // WHOLE: E is a multiple of 4, so that rows of d_scores are whole 16-byte chunks.  ACC: d_x is added to.
 template <bool BF16, int KS, int V, bool WHOLE, bool ACC>
-__global__ __launch_bounds__(GX_THREADS) void gate_x_kernel(GxArgs a) {
-  constexpr int B = BF16 ? 2 : 4;
+__global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxArgs a) {
+  using Tile = GxTile<BF16, KS>;
+  constexpr int B = BF16 ? 2 : 4, P = Tile::P, GT = Tile::GT, CPT = Tile::CPT, LOADS = Tile::LOADS, PITCH = Tile::PITCH;
+  __shared__ __align__(16) unsigned char pieces[2][P][GT * PITCH];
+  __shared__ uint32_t reals[2][GT / 4];              // a byte per token: it counts (ACC)
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
   const int d = a.d, E = a.E;
-  const int tile = static_cast<int>(blockIdx.x % a.tiles) * GX_WAVES + wave;
-  if (tile * 16 * V >= d) return;
-  const int col = tile * 16 * V + V * c;
-  const uint32_t begin = blockIdx.x / a.tiles * static_cast<uint32_t>(a.per_split);
+  int split, tile;                                   // as in gate_weight_kernel
+  if (a.splits % 8 == 0) {
+    tile = blockIdx.x / 8 % a.tiles;
+    split = blockIdx.x / 8 / a.tiles * 8 + blockIdx.x % 8;
+  } else {
+    tile = blockIdx.x % a.tiles;
+    split = blockIdx.x / a.tiles;
+  }
+  const int col = (tile * GX_WAVES + wave) * 16 * V + V * c;
+  const uint32_t begin = static_cast<uint32_t>(split) * a.per_split;
   const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
+  if (begin >= end) return;                          // the whole block
   const uint32_t pitch = static_cast<uint32_t>(d) * B, pitch_s = static_cast<uint32_t>(E) * 4;
-  struct Step {
-    float v[KS][8];
-    uint32_t mask;
-    GbRow<BF16, V> old[ACC ? 4 : 1];
-  };
-  // lane 16 g + c: experts 32 k + 8 g + 0..7 of token t0 + c; then tokens t0 + 4 g + 0..3 of its V columns
-  const uint32_t at_out = col < d ? 4 * g * pitch + static_cast<uint32_t>(col) * B : GB_NOWHERE;
-  auto load = [&](Step& s, uint32_t t0) {
-    const int rows = min(static_cast<int>(end - t0), 16);
+
+  // Chunk threadIdx.x + 256 i of a step: four experts of one token.
+  float v[LOADS][4];
+  uint32_t mask[LOADS];
+  auto load = [&](uint32_t t0) {
+    const int rows = min(static_cast<int>(end - t0), GT);
     const auto sr = gb_rows(a.d_scores + static_cast<int64_t>(t0) * E, rows, pitch_s);
-    s.mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? rows : 0, 1), c, 0, 0);
+    const auto mr = gb_rows(a.mask + t0, a.mask ? rows : 0, 1);
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const int e = 32 * k + 8 * g;
-      const uint32_t at = c * pitch_s + e * 4;
+    for (int i = 0; i < LOADS; ++i) {
+      const int at = threadIdx.x + GX_THREADS * i, row = at / CPT, e = at % CPT * 4;
+      mask[i] = __builtin_amdgcn_raw_buffer_load_b8(mr, row, 0, 0);
       if constexpr (WHOLE) {
+        const auto q = __builtin_amdgcn_raw_buffer_load_b128(sr, static_cast<int>(e < E ? row * pitch_s + e * 4 : GB_NOWHERE), 0, 0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const auto q = __builtin_amdgcn_raw_buffer_load_b128(sr, static_cast<int>(e + 4 * h < E ? at + 16 * h : GB_NOWHERE), 0, 0);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s.v[k][4 * h + j] = __uint_as_float(q[j]);
-        }
+        for (int j = 0; j < 4; ++j) v[i][j] = __uint_as_float(q[j]);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s.v[k][j] = gb_load_f32(sr, e + j < E ? at + 4 * j : GB_NOWHERE);
+        for (int j = 0; j < 4; ++j) v[i][j] = gb_load_f32(sr, e + j < E ? row * pitch_s + (e + j) * 4 : GB_NOWHERE);
       }
     }
-    if constexpr (ACC) {
-      const auto old = gb_rows(a.d_x + static_cast<int64_t>(t0) * pitch, rows, pitch);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) s.old[r].load(old, at_out + r * pitch);
-    }
-    __builtin_amdgcn_sched_barrier(0);
   };
-  uint32_t t0 = begin;
-  Step s0, s1;
-  load(s0, t0);
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int at = threadIdx.x + GX_THREADS * i, row = at / CPT, e = at % CPT * 4;
+      const bool real = !a.mask || mask[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = real ? v[i][j] : 0.f;
+      uint32_t q[3][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) gb_split(v[i][2 * u], v[i][2 * u + 1], q[0][u], q[1][u], q[2][u]);
+#pragma unroll
+      for (int p = 0; p < P; ++p) *reinterpret_cast<uint2*>(&pieces[buf][p][row * PITCH + e * 2]) = make_uint2(q[p][0], q[p][1]);
+      if (ACC && e == 0) reinterpret_cast<uint8_t*>(reals[buf])[row] = real;
+    }
+  };
+  load(begin);
   GbFrag<BF16, V> w[KS];
   {
     const uint32_t at = 8 * g * pitch + static_cast<uint32_t>(min(col, d - V)) * B;
@@ -452,62 +478,56 @@ __global__ __launch_bounds__(GX_THREADS) void gate_x_kernel(GxArgs a) {
       gb_transpose<BF16, V>(r, w[k]);
     }
   }
-  auto multiply = [&](const Step& s, uint32_t t0) {
-    const int rows = min(static_cast<int>(end - t0), 16);
-    const bool real = !a.mask || s.mask;
-    gb_f32x4 acc[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      uint32_t q[3][4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        gb_split(real ? s.v[k][2 * u] : 0.f, real ? s.v[k][2 * u + 1] : 0.f, q[0][u], q[1][u], q[2][u]);
-      const uint4 ah = make_uint4(q[0][0], q[0][1], q[0][2], q[0][3]), am = make_uint4(q[1][0], q[1][1], q[1][2], q[1][3]),
-                  al = make_uint4(q[2][0], q[2][1], q[2][2], q[2][3]);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if constexpr (!BF16) {
-          acc[i] = gb_mfma(al, w[k].f[0][i], acc[i]);
-          acc[i] = gb_mfma(ah, w[k].f[2][i], acc[i]);
-          acc[i] = gb_mfma(am, w[k].f[1][i], acc[i]);
-        }
-        acc[i] = gb_mfma(am, w[k].f[0][i], acc[i]);
-        if constexpr (!BF16) acc[i] = gb_mfma(ah, w[k].f[1][i], acc[i]);
-        acc[i] = gb_mfma(ah, w[k].f[0][i], acc[i]);
-      }
-    }
-    // padded tokens: zeros, or nothing where d_x is added to
-    const uint32_t keep = ACC ? static_cast<uint32_t>(__ballot(real)) : 0xFFFFu;       // bit i: token t0 + i counts
+  put(0);
+  __syncthreads();
+  // lane 16 g + c: tokens 4 g + 0..3 of every 16, its V columns
+  const uint32_t at_out = col < d ? 4 * g * pitch + static_cast<uint32_t>(col) * B : GB_NOWHERE;
+  int buf = 0;
+  for (uint32_t t0 = begin; t0 < end; t0 += GT, buf ^= 1) {
+    load(t0 + GT);                                   // behind the last step nothing is read
+    const int rows = min(static_cast<int>(end - t0), GT);
     const auto out = gb_rows(a.d_x + static_cast<int64_t>(t0) * pitch, rows, pitch);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      GbRow<BF16, V> o;
+    for (int m = 0; m < GT / 16; ++m) {
+      GbRow<BF16, V> old[ACC ? 4 : 1];
+      if constexpr (ACC) {
 #pragma unroll
-      for (int i = 0; i < o.W; ++i) {
-        if constexpr (BF16) {
-          float lo = acc[2 * i][r], hi = acc[2 * i + 1][r];
-          if constexpr (ACC) lo += bf16lo(s.old[r].w[i]), hi += bf16hi(s.old[r].w[i]);
-          o.w[i] = pack_bf16x2(lo, hi);
-        } else {
-          float v = acc[i][r];
-          if constexpr (ACC) v += __uint_as_float(s.old[r].w[i]);
-          o.w[i] = __float_as_uint(v);
-        }
+        for (int r = 0; r < 4; ++r) old[r].load(out, at_out + (16 * m + r) * pitch);
       }
-      o.store(out, keep >> (4 * g + r) & 1 ? at_out + r * pitch : GB_NOWHERE);
+      gb_f32x4 acc[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        // lane 16 g + c: experts 32 k + 8 g + 0..7 of token 16 m + c
+        const int at = (16 * m + c) * PITCH + 64 * k + 16 * g;
+        uint4 q[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) q[p] = *reinterpret_cast<const uint4*>(&pieces[buf][p][at]);
+        gb_products<BF16, BF16, V>(q[0], q[1], q[P - 1], w[k], acc);
+      }
+      uint32_t keep = 0x01010101u;                   // padded tokens: zeros, or nothing where d_x is added to
+      if constexpr (ACC) keep = reals[buf][4 * m + g];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        GbRow<BF16, V> o;
+#pragma unroll
+        for (int i = 0; i < o.W; ++i) {
+          if constexpr (BF16) {
+            float lo = acc[2 * i][r], hi = acc[2 * i + 1][r];
+            if constexpr (ACC) lo += bf16lo(old[r].w[i]), hi += bf16hi(old[r].w[i]);
+            o.w[i] = pack_bf16x2(lo, hi);
+          } else {
+            float s = acc[i][r];
+            if constexpr (ACC) s += __uint_as_float(old[r].w[i]);
+            o.w[i] = __float_as_uint(s);
+          }
+        }
+        o.store(out, keep >> (8 * r) & 1 ? at_out + (16 * m + r) * pitch : GB_NOWHERE);
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  while (t0 < end) {
-    load(s1, t0 + 16);
-    multiply(s0, t0);
-    t0 += 16;
-    if (t0 >= end) break;
-    load(s0, t0 + 16);
-    multiply(s1, t0);
-    t0 += 16;
+    put(buf ^ 1);
+    __syncthreads();
   }
 }
 
@@ -550,35 +570,36 @@ template <bool BF16, int MT, bool WHOLE> static int launch_weight(const GwPlan& 
   return MOE_OK;
 }
 
-template <bool BF16, int KS, int V> static void launch_x(const GxArgs& a, dim3 grid, hipStream_t st) {
+template <bool BF16, int KS, int V> static void launch_x(GxArgs a, bool accumulate, hipStream_t st) {
+  constexpr int GT = GxTile<BF16, KS>::GT, COLS = 16 * V * GX_WAVES;
+  a.tiles = (a.d + COLS - 1) / COLS;
+  const int64_t most = (static_cast<int64_t>(a.T) + GT - 1) / GT;
+  int64_t n = 1024 / a.tiles;
+  if (n > most) n = most;
+  if (n > 8) n = n / 8 * 8;
+  if (n < 1) n = 1;
+  int64_t per = (a.T + n - 1) / n;
+  per = (per + GT - 1) / GT * GT;
+  a.splits = static_cast<int>(n);
+  a.per_split = static_cast<int>(per);
   const bool whole = a.E % 4 == 0;
-  const auto kernel = a.accumulate ? (whole ? gate_x_kernel<BF16, KS, V, true, true> : gate_x_kernel<BF16, KS, V, false, true>)
-                                   : (whole ? gate_x_kernel<BF16, KS, V, true, false> : gate_x_kernel<BF16, KS, V, false, false>);
-  hipLaunchKernelGGL(kernel, grid, dim3(GX_THREADS), 0, st, a);
+  const auto kernel = accumulate ? (whole ? gate_x_kernel<BF16, KS, V, true, true> : gate_x_kernel<BF16, KS, V, false, true>)
+                                 : (whole ? gate_x_kernel<BF16, KS, V, true, false> : gate_x_kernel<BF16, KS, V, false, false>);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(a.tiles * a.splits)), dim3(GX_THREADS), 0, st, a);
 }
 
 template <bool BF16>
-static void x_grad(const moe_shape_t* s, const void* w, const float* ds, const uint8_t* mask, int accumulate, void* d_x, hipStream_t st) {
+static void x_grad(const moe_shape_t* s, const void* w, const float* ds, const uint8_t* mask, bool accumulate, void* d_x, hipStream_t st) {
   constexpr int V8 = BF16 ? 8 : 4, V4 = BF16 ? 4 : 2;
-  const int v = s->E <= 64 ? V8 : V4;
-  const int tiles = (s->d + 16 * v * GX_WAVES - 1) / (16 * v * GX_WAVES);
-  int64_t splits = 1024 / tiles;
-  const int64_t most = (static_cast<int64_t>(s->T) + 15) / 16;
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
-  int64_t per = (s->T + splits - 1) / splits;
-  per = (per + 15) / 16 * 16;
-  splits = (s->T + per - 1) / per;
-  const GxArgs a = {static_cast<const char*>(w), ds, mask, static_cast<char*>(d_x), s->T, s->d, s->E, tiles, static_cast<int>(per), accumulate};
-  const dim3 grid(static_cast<unsigned>(tiles * splits));
+  const GxArgs a = {static_cast<const char*>(w), ds, mask, static_cast<char*>(d_x), s->T, s->d, s->E, 0, 0, 0};
   if (s->E <= 32)
-    launch_x<BF16, 1, V8>(a, grid, st);
+    launch_x<BF16, 1, V8>(a, accumulate, st);
   else if (s->E <= 64)
-    launch_x<BF16, 2, V8>(a, grid, st);
+    launch_x<BF16, 2, V8>(a, accumulate, st);
   else if (s->E <= 128)
-    launch_x<BF16, 4, V4>(a, grid, st);
+    launch_x<BF16, 4, V4>(a, accumulate, st);
   else
-    launch_x<BF16, 8, V4>(a, grid, st);
+    launch_x<BF16, 8, V4>(a, accumulate, st);
 }
 
 template <bool BF16>
