@@ -40,6 +40,15 @@ __device__ __forceinline__ void gb_split(float a, float b, uint32_t& h, uint32_t
   l = pack_bf16x2(a - bf16lo(m), b - bf16hi(m));
 }
 
+// The pieces of eight values.
+__device__ __forceinline__ void gb_split8(const float (&v)[8], uint4 (&p)[3]) {
+  uint32_t q[3][4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) gb_split(v[2 * u], v[2 * u + 1], q[0][u], q[1][u], q[2][u]);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) p[i] = make_uint4(q[i][0], q[i][1], q[i][2], q[i][3]);
+}
+
 // The operand fragments of V column tiles from a lane's V columns of 8 rows along the reduction; P pieces each.
 template <bool BF16, int V> struct GbFrag {
   static constexpr int P = BF16 ? 1 : 3;
@@ -123,22 +132,8 @@ __device__ __forceinline__ void gb_products(uint4 h, uint4 m, uint4 l, const GbF
 // keep their own sums in registers and add them up in LDS at the end.  (Waves side by side over the columns would
 // share the pieces of d_scores, but leave eight times the sums to be written and read again: for 65536 tokens, d = 2048,
 // 64 experts half of what x itself has.)
-//
-// d_scores: of up to 32 experts a lane loads the values it needs (8 tokens of an expert) one by one; of 64 they come
-// 16 bytes at a time straight into LDS, as single loads would keep the address units longer than the HBM takes for x.
 constexpr int GW_WAVES = 8;
 constexpr int GW_THREADS = GW_WAVES * MOE_WAVE;
-constexpr int GW_STAGE = 32 * 64 * 4;                 // bytes of one step's d_scores in LDS: 32 tokens, 64 experts
-constexpr int GW_RED = GW_WAVES * 4 * MOE_WAVE * 16;  // bytes of the sums of the waves
-template <int MT> constexpr int GW_LDS = MT < 4 ? GW_RED : 2 * GW_WAVES * GW_STAGE;
-
-// What a wave multiplies in one step: 32 tokens, lane 16 g + c the tokens 8 g + 0..7 of its columns and experts.
-template <bool BF16, int MT, int V> struct GwStep {
-  GbRow<BF16, V> x[8];
-  float ds[MT < 4 ? MT : 1][8];
-  uint32_t mask;         // of token t0 + (lane & 31)
-  int left;              // tokens from t0 to the end, 32 at most
-};
 
 struct GwArgs {
   const char* x;
@@ -149,44 +144,35 @@ struct GwArgs {
   int T, d, E, tiles, splits, per_split, accumulate;
 };
 
-// Eight values of LDS, 256 bytes apart.  Written out, because in front of a read that it places itself the compiler waits
-// for every load into LDS, those for the next step as well.
-__device__ __forceinline__ void gb_read_column(uint32_t at, float (&v)[8]) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  f32x2 a, b, c, d;
-  asm volatile(
-      "ds_read2st64_b32 %0, %4 offset0:0 offset1:1\n\t"
-      "ds_read2st64_b32 %1, %4 offset0:2 offset1:3\n\t"
-      "ds_read2st64_b32 %2, %4 offset0:4 offset1:5\n\t"
-      "ds_read2st64_b32 %3, %4 offset0:6 offset1:7\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
-      : "v"(at)
-      : "memory");
-  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+// The block's place: column tile, group of experts, part of the tokens.  All tiles and groups of a part are on one XCD
+// (blocks are dealt to the 8 XCDs in turn): its L2 then gets d_scores once, and whole rows of x once.
+struct GwPlace {
+  int tile, chunk, split;
+};
+__device__ __forceinline__ GwPlace gw_place(int tiles, int chunks, int splits) {
+  const int n = tiles * chunks, b = blockIdx.x;
+  const int rest = splits % 8 == 0 ? b / 8 % n : b % n;
+  return {rest / chunks, rest % chunks, splits % 8 == 0 ? b / 8 / n * 8 + b % 8 : b / n};
 }
 
-template <int N> __device__ __forceinline__ void gb_wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// What a wave multiplies in one step: 32 tokens, lane 16 g + c the tokens 8 g + 0..7 of its columns and experts.
+template <bool BF16, int MT, int V> struct GwStep {
+  GbRow<BF16, V> x[8];
+  float ds[MT][8];
+  uint32_t mask;         // of token t0 + (lane & 31)
+  int left;              // tokens from t0 to the end
+};
 
-// WHOLE: E is a multiple of 4, so that rows of d_scores are whole 16-byte chunks (of use with MT = 4 only).
-template <bool BF16, int MT, int V, bool WHOLE>
-__device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char* lds, float (*red_b)[16 * MT]) {
+// Up to 32 experts: a lane loads the values of d_scores that it needs (8 tokens of an expert) one by one.
+template <bool BF16, int MT, int V>
+__global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(GwArgs a) {
   constexpr int B = BF16 ? 2 : 4;
-  constexpr bool STAGED = MT == 4;
+  __shared__ gb_f32x4 red[GW_WAVES][4][MOE_WAVE];
+  __shared__ float red_b[GW_WAVES][16 * MT];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
-  const int d = a.d, E = a.E, tiles = a.tiles, splits = a.splits;
-  // All column tiles and groups of experts of a token range on one XCD (blocks are dealt to the 8 XCDs in turn): its L2
-  // then gets d_scores once, and whole rows of x once.
-  const int chunks = (E + 16 * MT - 1) / (16 * MT);
-  int split, rest;
-  if (splits % 8 == 0) {
-    rest = blockIdx.x / 8 % (tiles * chunks);
-    split = blockIdx.x / 8 / (tiles * chunks) * 8 + blockIdx.x % 8;
-  } else {
-    rest = blockIdx.x % (tiles * chunks);
-    split = blockIdx.x / (tiles * chunks);
-  }
-  const int tile = rest / chunks, e0 = rest % chunks * 16 * MT;
+  const int d = a.d, E = a.E, splits = a.splits;
+  const GwPlace at_block = gw_place(a.tiles, 1, splits);
+  const int tile = at_block.tile, split = at_block.split;
   // (token numbers in 32 unsigned bits: T < 2^31, and no number passes it by more than the blocks' steps)
   const uint32_t begin = static_cast<uint32_t>(split) * a.per_split;
   const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
@@ -204,110 +190,68 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char
     for (int i = 0; i < V; ++i) acc[m][i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // STAGED: a row of 64 experts is 16 chunks of 16 bytes; chunk q of row r lies at place q ^ 4 (r / 8), so that the four
-  // lane groups, which read rows 8 apart, read different banks.
   using Step = GwStep<BF16, MT, V>;
-  constexpr int SLOADS = STAGED ? (WHOLE ? 8 : 32) : 8 * MT;
-  auto load = [&](Step& s, uint32_t t0, unsigned char* stage) {
-    s.left = min(static_cast<int>(end - t0), 32);
+  auto load = [&](Step& s, uint32_t t0) {
+    s.left = static_cast<int>(end - t0);
     // a descriptor for every row that the lanes have in common: what differs between lanes stays the same
     const char* x0 = a.x + static_cast<int64_t>(t0) * pitch;
     const char* s0 = reinterpret_cast<const char*>(a.d_scores) + static_cast<int64_t>(t0) * pitch_s;
-    s.mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? s.left : 0, 1), lane & 31, 0, 0);
-    if constexpr (STAGED) {
+    s.mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? min(s.left, 32) : 0, 1), lane & 31, 0, 0);
 #pragma unroll
-      for (int i = 0; i < SLOADS; ++i) {
-        if constexpr (WHOLE) {
-          const int e = min(e0 + 4 * (c ^ 4 * (i / 2)), E - 4);
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(gb_rows(s0 + 4 * i * pitch_s, s.left - 4 * i, pitch_s),
-                                                   (__attribute__((address_space(3))) void*)(stage + i * 1024), 16,
-                                                   static_cast<int>(g * pitch_s + e * 4), 0, 0, 0);
-        } else {
-          const int e = min(e0 + (lane ^ 16 * (i / 8)), E - 1);
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(gb_rows(s0 + i * pitch_s, s.left - i, pitch_s),
-                                                   (__attribute__((address_space(3))) void*)(stage + i * 256), 4,
-                                                   static_cast<int>(e * 4), 0, 0, 0);
-        }
-      }
-    } else {
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int j = 0; j < 8; ++j)
+        s.ds[m][j] = gb_load_f32(gb_rows(s0 + j * pitch_s, min(s.left, 32) - j, pitch_s),
+                                 8 * g * pitch_s + static_cast<uint32_t>(min(16 * m + c, E - 1)) * 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          s.ds[m][j] = gb_load_f32(gb_rows(s0 + j * pitch_s, s.left - j, pitch_s),
-                                   8 * g * pitch_s + static_cast<uint32_t>(min(e0 + 16 * m + c, E - 1)) * 4);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s.x[j].load(gb_rows(x0 + static_cast<int64_t>(j) * pitch, with_w ? s.left - j : 0, pitch), at_x);
+    for (int j = 0; j < 8; ++j) s.x[j].load(gb_rows(x0 + static_cast<int64_t>(j) * pitch, with_w ? min(s.left, 32) - j : 0, pitch), at_x);
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto multiply = [&](Step& s, uint32_t stage_at) {
-    // the loads of the step that follows were issued last: all but those have arrived
-    gb_wait_loads<SLOADS + 8 + 1>();
-    uint32_t real = 0xFFu;                           // bit j: token t0 + 8 g + j counts
-    const bool some = a.mask || s.left < 32;
-    if (some) {
-      real = static_cast<uint32_t>(__ballot((lane & 31) < s.left && (!a.mask || s.mask))) >> (8 * g);
+  auto multiply = [&](Step& s) {
+    if (a.mask || s.left < 32) {
+      // bit j: token t0 + 8 g + j counts
+      const uint32_t real = static_cast<uint32_t>(__ballot((lane & 31) < s.left && (!a.mask || s.mask))) >> (8 * g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s.x[j].keep(real >> j & 1);
+      for (int j = 0; j < 8; ++j) {
+        s.x[j].keep(real >> j & 1);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) s.ds[m][j] = real >> j & 1 ? s.ds[m][j] : 0.f;
+      }
     }
     GbFrag<BF16, V> b;
     gb_transpose<BF16, V>(s.x, b);
-    asm volatile("" : "+v"(stage_at));               // addresses are made anew in every step, not kept in registers
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      float v[8];
-      if constexpr (STAGED) {
-        gb_read_column(stage_at ^ 64 * m, v);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = s.ds[m][j];
-      }
-      if (some) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = real >> j & 1 ? v[j] : 0.f;
-      }
       if (with_bias) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bias[m] += v[j];
+        for (int j = 0; j < 8; ++j) bias[m] += s.ds[m][j];
       }
-      uint32_t q[3][4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) gb_split(v[2 * u], v[2 * u + 1], q[0][u], q[1][u], q[2][u]);
-      const uint4 ah = make_uint4(q[0][0], q[0][1], q[0][2], q[0][3]), am = make_uint4(q[1][0], q[1][1], q[1][2], q[1][3]),
-                  al = make_uint4(q[2][0], q[2][1], q[2][2], q[2][3]);
-      gb_products<BF16, false, V>(ah, am, al, b, acc[m]);
+      uint4 p[3];
+      gb_split8(s.ds[m], p);
+      gb_products<BF16, false, V>(p[0], p[1], p[2], b, acc[m]);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
   // the next step's operands are on their way while this one's are multiplied; behind the last step nothing is read
   {
-    unsigned char* stage0 = lds + wave * 2 * GW_STAGE;
-    unsigned char* stage1 = stage0 + GW_STAGE;
-    // where this lane finds expert c of the first of its 8 tokens; expert 16 m + c: 64 m in bits 6 and 7, by the places of
-    // the chunks (stages start at multiples of 256)
-    const uint32_t at0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)stage0)) + 2048 * g + 64 * g + 4 * c;
     Step s0, s1;
     uint32_t t0 = begin + 32 * wave;
-    load(s0, t0, stage0);
+    load(s0, t0);
     while (t0 < end) {
-      load(s1, t0 + 32 * GW_WAVES, stage1);
-      multiply(s0, at0);
+      load(s1, t0 + 32 * GW_WAVES);
+      multiply(s0);
       t0 += 32 * GW_WAVES;
       if (t0 >= end) break;
-      load(s0, t0 + 32 * GW_WAVES, stage0);
-      multiply(s1, at0 + GW_STAGE);
+      load(s0, t0 + 32 * GW_WAVES);
+      multiply(s1);
       t0 += 32 * GW_WAVES;
     }
-    gb_wait_loads<0>();                              // LDS is free for the sums
   }
-  __syncthreads();
 
   // sums of the waves, 16 experts at a time: lane 16 g + c of a wave holds experts 4 g + 0..3 of the columns V c + i
   const int64_t n = static_cast<int64_t>(E) * d;
   float* to = a.out_w + (splits > 1 ? split * n : 0);
   const bool add = a.accumulate && splits == 1;
-  auto red = reinterpret_cast<gb_f32x4(*)[4][MOE_WAVE]>(lds);
   if (with_w) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -318,7 +262,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char
         for (int i = 0; i < 4; ++i) red[wave][i][lane] = acc[m][4 * quad + i];
         __syncthreads();
         const int cc = threadIdx.x & 15, row = threadIdx.x >> 4;
-        const int e = e0 + 16 * m + row, at = tile * 16 * V + V * cc + 4 * quad;
+        const int e = 16 * m + row, at = tile * 16 * V + V * cc + 4 * quad;
         if (row < 16 && e < E && at < d) {
           const int from = row / 4 * 16 + cc;
           float4* o = reinterpret_cast<float4*>(to + static_cast<int64_t>(e) * d + at);
@@ -343,7 +287,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char
       if (g == 0) red_b[wave][16 * m + c] = v;
     }
     __syncthreads();
-    const int e = e0 + threadIdx.x;
+    const int e = threadIdx.x;
     if (threadIdx.x < 16 * MT && e < E) {
       float v = add ? a.out_b[e] : 0.f;
       for (int w = 0; w < GW_WAVES; ++w) v += red_b[w][threadIdx.x];
@@ -352,35 +296,207 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, unsigned char
   }
 }
 
-template <bool BF16, int MT, int V, bool WHOLE>
-__global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(GwArgs a) {
-  extern __shared__ __align__(256) unsigned char lds[];
-  __shared__ float red_b[GW_WAVES][16 * MT];
-  gate_weight_block<BF16, MT, V, WHOLE>(a, lds, red_b);
+// More than 32 experts, 64 of them and 64 V columns to a block: its waves lie side by side over the columns, four for the
+// first 32 tokens of a step and four for the next, and share the pieces of d_scores, which the block makes once and keeps
+// in LDS in the order in which the lanes want them: thread 64 w + i of a step cuts 8 tokens (8 (w % 4) of half w / 4) of
+// expert i.
+constexpr int GWW_PIECES = 4 * MOE_WAVE * 16;         // bytes of a piece of 32 tokens, 64 experts
+constexpr int GWW_STEP = 2 * 3 * GWW_PIECES;
+constexpr int GWW_LDS = 2 * GWW_STEP > GW_WAVES * 8 * MOE_WAVE * 16 ? 2 * GWW_STEP : GW_WAVES * 8 * MOE_WAVE * 16;
+
+template <bool BF16, int V>
+__device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned char* lds, float* red_b) {
+  constexpr int B = BF16 ? 2 : 4, MT = 4;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
+  const int half = wave >> 2;
+  const int d = a.d, E = a.E, splits = a.splits;
+  const GwPlace place = gw_place(a.tiles, (E + 63) / 64, splits);
+  const int e0 = place.chunk * 64;
+  const uint32_t begin = static_cast<uint32_t>(place.split) * a.per_split;
+  const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
+  const uint32_t pitch = static_cast<uint32_t>(d) * B, pitch_s = static_cast<uint32_t>(E) * 4;
+  const int col = (place.tile * 4 + (wave & 3)) * 16 * V + V * c;
+  const uint32_t at_x = 8 * g * pitch + static_cast<uint32_t>(min(col, d - V)) * B;
+  const bool with_w = a.out_w, with_bias = a.out_b && place.tile == 0;
+
+  // this thread's part of d_scores: 8 tokens of an expert
+  const uint32_t at_s = 8 * (wave & 3) * pitch_s + static_cast<uint32_t>(min(e0 + lane, E - 1)) * 4;
+  const int at_piece = half * 3 * GWW_PIECES + (lane / 16 * MOE_WAVE + 16 * (wave & 3) + lane % 16) * 16;
+  float ds[8], bias = 0.f;
+  GbRow<BF16, V> x[8];
+  uint32_t mask;
+  auto load = [&](uint32_t t0) {
+    const int left = static_cast<int>(end - t0) - 32 * half;
+    const int64_t t = static_cast<int64_t>(t0) + 32 * half;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      ds[j] = gb_load_f32(gb_rows(reinterpret_cast<const char*>(a.d_scores) + (t + j) * pitch_s, min(left, 32) - j, pitch_s), at_s);
+    mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t, a.mask ? min(left, 32) : 0, 1), lane & 31, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j].load(gb_rows(a.x + (t + j) * pitch, with_w ? min(left, 32) - j : 0, pitch), at_x);
+  };
+  // bit i: token t0 + 32 half + i counts
+  auto reals = [&](uint32_t t0) {
+    const int left = static_cast<int>(end - t0) - 32 * half;
+    return static_cast<uint32_t>(__ballot((lane & 31) < left && (!a.mask || mask)));
+  };
+  auto some_padded = [&](uint32_t t0) { return a.mask || static_cast<int>(end - t0) < 64; };
+  auto put = [&](uint32_t t0, unsigned char* to) {
+    if (some_padded(t0)) {
+      const uint32_t real = reals(t0) >> (8 * (wave & 3));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ds[j] = real >> j & 1 ? ds[j] : 0.f;
+    }
+    if (with_bias) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) bias += ds[j];
+    }
+    uint4 p[3];
+    gb_split8(ds, p);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + at_piece + q * GWW_PIECES) = p[q];
+  };
+
+  gb_f32x4 acc[MT][V];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[m][i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
+  // A step's operands go over to the registers that the products read, and the next step's are requested into the ones
+  // that are free then; behind the last step nothing is read.
+  load(begin);
+  put(begin, lds);
+  __syncthreads();
+  uint32_t at_lds = 0;
+  for (uint32_t t0 = begin; t0 < end; at_lds = GWW_STEP - at_lds) {
+    if (some_padded(t0)) {
+      const uint32_t real = reals(t0) >> (8 * g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j].keep(real >> j & 1);
+    }
+    GbFrag<BF16, V> b;
+    gb_transpose<BF16, V>(x, b);
+    __builtin_amdgcn_sched_barrier(0);
+    t0 += 64;
+    load(t0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      uint4 p[3];
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        p[q] = *reinterpret_cast<const uint4*>(lds + at_lds + (half * 3 + q) * GWW_PIECES + (m * MOE_WAVE + lane) * 16);
+      gb_products<BF16, false, V>(p[0], p[1], p[2], b, acc[m]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    put(t0, lds + (GWW_STEP - at_lds));
+    __syncthreads();
+  }
+
+  // The halves' sums meet in LDS: the first half's waves finish the experts 0..31, the second's 32..63.
+  const int64_t n = static_cast<int64_t>(E) * d;
+  float* to = a.out_w + (splits > 1 ? place.split * n : 0);
+  const bool add = a.accumulate && splits == 1;
+  auto red = reinterpret_cast<gb_f32x4(*)[V][MOE_WAVE]>(lds);
+  auto finish = [&](const gb_f32x4 (&mine)[V], int m) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int e = e0 + 16 * m + 4 * g + r;
+      if (e >= E || col >= d) continue;
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        float4* o = reinterpret_cast<float4*>(to + static_cast<int64_t>(e) * d + col + i);
+        float4 s = add ? *o : make_float4(0.f, 0.f, 0.f, 0.f);
+        s.x += mine[i][r], s.y += mine[i + 1][r], s.z += mine[i + 2][r], s.w += mine[i + 3][r];
+        *o = s;
+      }
+    }
+  };
+  if (with_w) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (q > 0) __syncthreads();
+      if (half == 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[wave][i][lane] = acc[2 + q][i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[wave][i][lane] = acc[q][i];
+      }
+      __syncthreads();
+      if (half == 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[q][i] += red[wave + 4][i][lane];
+        finish(acc[q], q);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[2 + q][i] += red[wave - 4][i][lane];
+        finish(acc[2 + q], 2 + q);
+      }
+    }
+  }
+  if (with_bias) {
+    red_b[threadIdx.x] = bias;
+    __syncthreads();
+    const int e = e0 + threadIdx.x;
+    if (threadIdx.x < 64 && e < E) {
+      float v = add ? a.out_b[e] : 0.f;
+      for (int w = 0; w < GW_WAVES; ++w) v += red_b[64 * w + threadIdx.x];
+      a.out_b[(splits > 1 ? static_cast<int64_t>(place.split) * E : 0) + e] = v;
+    }
+  }
 }
 
-// out[i] (+)= the sum of the parts' elements i, in order; four consecutive ones per thread.
+template <bool BF16, int V>
+__global__ __launch_bounds__(GW_THREADS) void gate_weight_wide_kernel(GwArgs a) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ float red_b[GW_THREADS];
+  gate_weight_wide_block<BF16, V>(a, lds, red_b);
+}
+
+// out[i] (+)= the sum of the parts' elements i: four consecutive ones per thread, every fourth part, eight of them on
+// their way at a time; the four sums of an element meet in LDS.  The order of the additions is fixed.
 constexpr int GS_THREADS = 256;
-__global__ __launch_bounds__(GS_THREADS) void gate_sum_kernel(const float* __restrict__ part_w, float* __restrict__ out_w, int64_t n,
-                                                              const float* __restrict__ part_b, float* __restrict__ out_b, int E,
-                                                              int splits, int accumulate) {
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * GS_THREADS + threadIdx.x) * 4;
-  if (out_w && i < n) {
-    float4* o = reinterpret_cast<float4*>(out_w + i);
-    float4 s = accumulate ? *o : make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p = 0; p < splits; ++p) {
-      const float4 v = *reinterpret_cast<const float4*>(part_w + p * n + i);
-      s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+constexpr int GS_GROUPS = 4;
+constexpr int GS_COLUMNS = GS_THREADS / GS_GROUPS;
+__device__ __forceinline__ float4 gs_add(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ float gs_add(float a, float b) { return a + b; }
+template <class V> __device__ __forceinline__ void gs_column(const V* part, V* out, int64_t n, int64_t i, int splits, int accumulate, V* lds) {
+  const int column = threadIdx.x % GS_COLUMNS, group = threadIdx.x / GS_COLUMNS;
+  V s{};
+  if (i < n) {
+    for (int p = group; p < splits; p += 8 * GS_GROUPS) {
+      V v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        v[u] = V{};
+        if (p + u * GS_GROUPS < splits) v[u] = part[(p + u * GS_GROUPS) * n + i];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s = gs_add(s, v[u]);
     }
-    *o = s;
   }
-  if (out_b && blockIdx.x == 0 && static_cast<int>(threadIdx.x) < E) {
-    float s = accumulate ? out_b[threadIdx.x] : 0.f;
-    for (int p = 0; p < splits; ++p) s += part_b[static_cast<int64_t>(p) * E + threadIdx.x];
-    out_b[threadIdx.x] = s;
+  if (group > 0) lds[(group - 1) * GS_COLUMNS + column] = s;
+  __syncthreads();
+  if (group == 0 && i < n) {
+#pragma unroll
+    for (int u = 0; u < GS_GROUPS - 1; ++u) s = gs_add(s, lds[u * GS_COLUMNS + column]);
+    out[i] = accumulate ? gs_add(s, out[i]) : s;
   }
 }
-static_assert(GS_THREADS >= MOE_MAX_E, "one thread per expert");
+// Blocks: the first blocks_w for d_w_gate (n elements), the others for d_gate_bias.
+__global__ __launch_bounds__(GS_THREADS) void gate_sum_kernel(const float* __restrict__ part_w, float* __restrict__ out_w, int64_t n,
+                                                              int blocks_w, const float* __restrict__ part_b,
+                                                              float* __restrict__ out_b, int E, int splits, int accumulate) {
+  __shared__ float4 lds[(GS_GROUPS - 1) * GS_COLUMNS];
+  const int column = threadIdx.x % GS_COLUMNS, block = blockIdx.x;
+  if (block < blocks_w)
+    gs_column(reinterpret_cast<const float4*>(part_w), reinterpret_cast<float4*>(out_w), n / 4,
+              static_cast<int64_t>(block) * GS_COLUMNS + column, splits, accumulate, lds);
+  else
+    gs_column(part_b, out_b, static_cast<int64_t>(E), static_cast<int64_t>(block - blocks_w) * GS_COLUMNS + column, splits, accumulate,
+              reinterpret_cast<float*>(lds));
+}
 
 // ------------------------------------------------------------------------------------------------ hidden states' gradient
 // A wave keeps the fragments of w_gate of its 16 V columns (KS steps of 32 experts) in registers; the four waves of a
@@ -535,22 +651,24 @@ __global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxAr
 // Blocks of the weights' gradient: column tiles, groups of experts, and parts of the tokens, of which there are as many
 // as fill the chip twice, each of 32 tokens per wave or more.
 struct GwPlan {
-  int mt, v, tiles, chunks, splits, per_split;
+  int mt, tiles, chunks, splits, per_split;
 };
 static GwPlan gw_plan(const moe_shape_t* s) {
   GwPlan p{};
   p.mt = s->E <= 16 ? 1 : s->E <= 32 ? 2 : 4;
-  p.v = s->dtype == MOE_F32 ? 4 : 8;
-  p.tiles = (s->d + 16 * p.v - 1) / (16 * p.v);
-  p.chunks = (s->E + 16 * p.mt - 1) / (16 * p.mt);
-  const int64_t most = (static_cast<int64_t>(s->T) + 32 * GW_WAVES - 1) / (32 * GW_WAVES);
+  const int v = s->dtype == MOE_F32 ? 4 : 8, cols = 16 * v * (p.mt == 4 ? 4 : 1);
+  p.tiles = (s->d + cols - 1) / cols;
+  p.chunks = p.mt == 4 ? (s->E + 63) / 64 : 1;
+  const int step = p.mt == 4 ? 64 : 32 * GW_WAVES;
+  const int64_t most = (static_cast<int64_t>(s->T) + step - 1) / step;
   int64_t n = (p.mt == 4 ? 256 : 512) / (static_cast<int64_t>(p.tiles) * p.chunks);
   if (n > most) n = most;
   if (n > 8) n = n / 8 * 8;
   if (n < 1) n = 1;
   int64_t per = (s->T + n - 1) / n;
-  per = (per + 31) / 32 * 32;
-  p.per_split = static_cast<int>(per < 32 ? 32 : per);
+  const int unit = p.mt == 4 ? 64 : 32;
+  per = (per + unit - 1) / unit * unit;
+  p.per_split = static_cast<int>(per < unit ? unit : per);
   p.splits = static_cast<int>(n);
   return p;
 }
@@ -560,13 +678,20 @@ size_t gate_backward_workspace_bytes(const moe_shape_t* shape) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * shape->E * (static_cast<size_t>(shape->d) + 1) * sizeof(float) : 0;
 }
 
-template <bool BF16, int MT, bool WHOLE> static int launch_weight(const GwPlan& p, const GwArgs& a, hipStream_t st) {
+template <bool BF16> static int launch_weight(const GwPlan& p, const GwArgs& a, hipStream_t st) {
   constexpr int V = BF16 ? 8 : 4;
-  const auto kernel = gate_weight_kernel<BF16, MT, V, WHOLE>;
-  static LdsOnce once;
-  const int rc = ensure_dynamic_lds(once, reinterpret_cast<const void*>(kernel), GW_LDS<MT>);
-  if (rc != MOE_OK) return rc;
-  hipLaunchKernelGGL(kernel, dim3(p.tiles * p.chunks * p.splits), dim3(GW_THREADS), GW_LDS<MT>, st, a);
+  const dim3 grid(static_cast<unsigned>(p.tiles * p.chunks * p.splits));
+  if (p.mt == 1) {
+    hipLaunchKernelGGL((gate_weight_kernel<BF16, 1, V>), grid, dim3(GW_THREADS), 0, st, a);
+  } else if (p.mt == 2) {
+    hipLaunchKernelGGL((gate_weight_kernel<BF16, 2, V>), grid, dim3(GW_THREADS), 0, st, a);
+  } else {
+    const auto kernel = gate_weight_wide_kernel<BF16, V>;
+    static LdsOnce once;
+    const int rc = ensure_dynamic_lds(once, reinterpret_cast<const void*>(kernel), GWW_LDS);
+    if (rc != MOE_OK) return rc;
+    hipLaunchKernelGGL(kernel, grid, dim3(GW_THREADS), GWW_LDS, st, a);
+  }
   return MOE_OK;
 }
 
@@ -613,13 +738,13 @@ static int gate_backward(const moe_shape_t* shape, const void* x, const void* w_
     float* part_b = part + p.splits * n;
     const GwArgs a = {static_cast<const char*>(x), d_scores, mask, d_w_gate ? (parts ? part : d_w_gate) : nullptr,
                       d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, shape->T, shape->d, shape->E, p.tiles, p.splits, p.per_split, acc_w};
-    const int rc = p.mt == 1 ? launch_weight<BF16, 1, true>(p, a, st) : p.mt == 2 ? launch_weight<BF16, 2, true>(p, a, st)
-                 : shape->E % 4 == 0 ? launch_weight<BF16, 4, true>(p, a, st) : launch_weight<BF16, 4, false>(p, a, st);
+    const int rc = launch_weight<BF16>(p, a, st);
     if (rc != MOE_OK) return rc;
     if (parts) {
-      const int64_t threads = d_w_gate ? n / 4 : 1;
-      hipLaunchKernelGGL(gate_sum_kernel, dim3(static_cast<unsigned>((threads + GS_THREADS - 1) / GS_THREADS)), dim3(GS_THREADS), 0, st, part,
-                         d_w_gate, n, part_b, d_gate_bias, shape->E, p.splits, acc_w);
+      const int blocks_w = d_w_gate ? static_cast<int>((n / 4 + GS_COLUMNS - 1) / GS_COLUMNS) : 0;
+      const int blocks_b = d_gate_bias ? (shape->E + GS_COLUMNS - 1) / GS_COLUMNS : 0;
+      hipLaunchKernelGGL(gate_sum_kernel, dim3(static_cast<unsigned>(blocks_w + blocks_b)), dim3(GS_THREADS), 0, st, part, d_w_gate, n,
+                         blocks_w, part_b, d_gate_bias, shape->E, p.splits, acc_w);
     }
   }
   if (d_x && shape->T > 0) x_grad<BF16>(shape, w_gate, d_scores, mask, acc_x, d_x, st);
