@@ -30,10 +30,9 @@ struct GradPiece {
   bool bf16;
 };
 
-// The piece of this block: the last tensor whose first block is not behind it (tensors without elements have no block).
-__device__ __forceinline__ GradPiece grad_piece(const GradTable& tab, int count, int64_t piece) {
+// Piece b of the table: of the last tensor whose first block is not behind it (tensors without elements have no block).
+__device__ __forceinline__ GradPiece grad_piece(const GradTable& tab, int count, int64_t piece, int b) {
   int lo = 0, hi = count - 1;
-  const int b = blockIdx.x;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
     if (tab.first[mid] <= b) lo = mid; else hi = mid - 1;
@@ -48,56 +47,124 @@ __device__ __forceinline__ GradPiece grad_piece(const GradTable& tab, int count,
   return g;
 }
 
-__device__ __forceinline__ float grad_load(const void* p, int64_t i, bool bf16) {
-  return bf16 ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+// The elements [begin, end) of a tensor: those in whole, aligned 16-byte chunks by `chunk`(pointer to it, its first
+// element's number), the others, at most 7 at either end, by `one`(number).
+template <bool BF16, class Chunk, class One>
+__device__ __forceinline__ void grad_for_each(const GradPiece& g, Chunk chunk, One one) {
+  constexpr int PER = BF16 ? 8 : 4, UNROLL = 4;
+  const int64_t skip = -static_cast<int64_t>(reinterpret_cast<uintptr_t>(g.data) / (16 / PER)) & (PER - 1);   // elements before an aligned one
+  int64_t first = (g.begin - skip + PER - 1) / PER * PER + skip, last = (g.end - skip) / PER * PER + skip;
+  if (g.begin <= skip) first = skip;
+  if (first >= last) first = last = g.end;
+  if (g.begin + threadIdx.x < first) one(g.begin + threadIdx.x);
+  if (last + threadIdx.x < g.end) one(last + threadIdx.x);
+  const int64_t n = (last - first) / PER;
+  const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(g.data) + first * (16 / PER));
+  int64_t i = threadIdx.x;
+  for (; i + (UNROLL - 1) * GR_THREADS < n; i += UNROLL * GR_THREADS) {
+    uint4 v[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) v[u] = p[i + u * GR_THREADS];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) chunk(v[u], first + (i + u * GR_THREADS) * PER);
+  }
+  for (; i < n; i += GR_THREADS) chunk(p[i], first + i * PER);
 }
 
+// Sum over the block, in a fixed order, on every thread.
 __device__ __forceinline__ double grad_block_sum(double v, double* lds) {
-  lds[threadIdx.x] = v;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  if (lane_id() == 0) lds[threadIdx.x / MOE_WAVE] = v;
   __syncthreads();
-  for (int half = GR_THREADS / 2; half >= 1; half >>= 1) {
-    if (threadIdx.x < static_cast<unsigned>(half)) lds[threadIdx.x] += lds[threadIdx.x + half];
-    __syncthreads();
-  }
-  return lds[0];
+  v = 0.0;
+#pragma unroll
+  for (int w = 0; w < GR_THREADS / MOE_WAVE; ++w) v += lds[w];
+  return v;
+}
+
+template <bool BF16> __device__ __forceinline__ double grad_squares(const GradPiece& g) {
+  double s[4] = {};
+  auto add = [&](int k, float f) {
+    const double d = f;
+    s[k & 3] = fma(d, d, s[k & 3]);
+  };
+  grad_for_each<BF16>(
+      g,
+      [&](uint4 v, int64_t) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (BF16) {
+            add(2 * k, bf16lo(w[k]));
+            add(2 * k + 1, bf16hi(w[k]));
+          } else {
+            add(k, __uint_as_float(w[k]));
+          }
+        }
+      },
+      [&](int64_t i) { add(0, BF16 ? bf16_to_f32(static_cast<const bf16_t*>(g.data)[i]) : static_cast<const float*>(g.data)[i]); });
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 __global__ __launch_bounds__(GR_THREADS) void grad_square_kernel(GradTable tab, int count, int64_t piece, double* __restrict__ part) {
-  __shared__ double lds[GR_THREADS];
-  const GradPiece g = grad_piece(tab, count, piece);
-  double s = 0.0;
-  for (int64_t i = g.begin + threadIdx.x; i < g.end; i += GR_THREADS) {
-    const double v = grad_load(g.data, i, g.bf16);
-    s = fma(v, v, s);
-  }
-  s = grad_block_sum(s, lds);
+  __shared__ double lds[GR_THREADS / MOE_WAVE];
+  const GradPiece g = grad_piece(tab, count, piece, blockIdx.x);
+  const double s = grad_block_sum(g.bf16 ? grad_squares<true>(g) : grad_squares<false>(g), lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// coef[0] = min(1, max_norm / norm); 1 where the norm is no finite number (the caller sees it in `norm`).
-__global__ __launch_bounds__(GR_THREADS) void grad_finish_kernel(const double* __restrict__ part, int64_t pieces, double max_norm,
-                                                                 float* __restrict__ norm, float* __restrict__ coef) {
-  __shared__ double lds[GR_THREADS];
+// The norm from the pieces' sums, the same on every thread of every block.
+__device__ __forceinline__ double grad_total_norm(const double* __restrict__ part, int64_t pieces, double* lds) {
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < pieces; i += GR_THREADS) s += part[i];
-  s = sqrt(grad_block_sum(s, lds));
-  if (threadIdx.x == 0) {
-    *norm = static_cast<float>(s);
-    *coef = s > max_norm && s < INFINITY ? static_cast<float>(max_norm / s) : 1.f;
-  }
+  return sqrt(grad_block_sum(s, lds));
 }
 
-__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, int count, int64_t piece, const float* __restrict__ coef) {
-  const GradPiece g = grad_piece(tab, count, piece);
-  const float c = *coef;
-  if (c == 1.f && g.out == g.data) return;
-  for (int64_t i = g.begin + threadIdx.x; i < g.end; i += GR_THREADS) {
-    const float v = grad_load(g.data, i, g.bf16) * c;
-    if (g.bf16)
-      static_cast<bf16_t*>(g.out)[i] = f32_to_bf16(v);
+__global__ __launch_bounds__(GR_THREADS) void grad_finish_kernel(const double* __restrict__ part, int64_t pieces, float* __restrict__ norm) {
+  __shared__ double lds[GR_THREADS / MOE_WAVE];
+  const double s = grad_total_norm(part, pieces, lds);
+  if (threadIdx.x == 0) *norm = static_cast<float>(s);
+}
+
+template <bool BF16> __device__ __forceinline__ void grad_scale(const GradPiece& g, float c) {
+  auto one = [&](int64_t i) {
+    if constexpr (BF16)
+      static_cast<bf16_t*>(g.out)[i] = f32_to_bf16(bf16_to_f32(static_cast<const bf16_t*>(g.data)[i]) * c);
     else
-      static_cast<float*>(g.out)[i] = v;
+      static_cast<float*>(g.out)[i] = static_cast<const float*>(g.data)[i] * c;
+  };
+  if ((reinterpret_cast<uintptr_t>(g.out) ^ reinterpret_cast<uintptr_t>(g.data)) & 15) {   // no common alignment
+    for (int64_t i = g.begin + threadIdx.x; i < g.end; i += GR_THREADS) one(i);
+    return;
   }
+  grad_for_each<BF16>(
+      g,
+      [&](uint4 v, int64_t i) {
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          w[k] = BF16 ? pack_bf16x2(bf16lo(w[k]) * c, bf16hi(w[k]) * c) : __float_as_uint(__uint_as_float(w[k]) * c);
+        nt_store(reinterpret_cast<uint4*>(static_cast<char*>(g.out) + i * (BF16 ? 2 : 4)), make_uint4(w[0], w[1], w[2], w[3]));
+      },
+      one);
+}
+
+// Every block makes the factor from the pieces' sums by itself, which saves a launch.  The pieces are taken from the last
+// to the first: those that the norm's pass read last are in the memory-side cache.
+__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, int count, int64_t piece, const double* __restrict__ part,
+                                                                int64_t pieces, double max_norm, float* __restrict__ norm) {
+  __shared__ double lds[GR_THREADS / MOE_WAVE];
+  const double s = grad_total_norm(part, pieces, lds);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(s);
+  // 1 where the norm is no finite number: the caller sees it in `norm`
+  const float c = s > max_norm && s < INFINITY ? static_cast<float>(max_norm / s) : 1.f;
+  const GradPiece g = grad_piece(tab, count, piece, gridDim.x - 1 - blockIdx.x);
+  if (c == 1.f && g.out == g.data) return;
+  if (g.bf16)
+    grad_scale<true>(g, c);
+  else
+    grad_scale<false>(g, c);
 }
 
 static int check_grads(int32_t count, const moe_tensor_t* tensors, bool with_out) {
@@ -158,19 +225,19 @@ static int grads_call(int32_t count, const moe_tensor_t* tensors, bool clip, dou
   if (!norm || (reinterpret_cast<uintptr_t>(norm) & 3) || !workspace || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
   int64_t piece = 0;
   const int64_t pieces = grad_pieces(count, tensors, &piece);
-  if (workspace_bytes < static_cast<size_t>(pieces) * 8 + 16) return MOE_ERR_WORKSPACE;
-  float* coef = static_cast<float*>(workspace);
-  double* part = static_cast<double*>(workspace) + 2;
+  if (workspace_bytes < static_cast<size_t>(pieces) * 8) return MOE_ERR_WORKSPACE;
+  double* part = static_cast<double*>(workspace);
   int64_t at = 0;
   for_tables(count, tensors, piece, [&](const GradTable& tab, int n, int blocks) {
     hipLaunchKernelGGL(grad_square_kernel, dim3(blocks), dim3(GR_THREADS), 0, st, tab, n, piece, part + at);
     at += blocks;
   });
-  hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(GR_THREADS), 0, st, part, pieces, max_norm, norm, coef);
-  if (clip)
+  if (clip && pieces > 0)
     for_tables(count, tensors, piece, [&](const GradTable& tab, int n, int blocks) {
-      hipLaunchKernelGGL(grad_scale_kernel, dim3(blocks), dim3(GR_THREADS), 0, st, tab, n, piece, coef);
+      hipLaunchKernelGGL(grad_scale_kernel, dim3(blocks), dim3(GR_THREADS), 0, st, tab, n, piece, part, pieces, max_norm, norm);
     });
+  else
+    hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(GR_THREADS), 0, st, part, pieces, norm);
   return launch_status();
 }
 
@@ -181,7 +248,8 @@ extern "C" int moe_grad_workspace_bytes(int32_t count, const moe_tensor_t* tenso
   if (rc != MOE_OK) return rc;
   if (!out_bytes) return MOE_ERR_INVALID_ARG;
   int64_t piece = 0;
-  *out_bytes = (static_cast<size_t>(moe::grad_pieces(count, tensors, &piece)) * 8 + 16 + 255) / 256 * 256;
+  *out_bytes = (static_cast<size_t>(moe::grad_pieces(count, tensors, &piece)) * 8 + 255) / 256 * 256;
+  if (*out_bytes == 0) *out_bytes = 256;
   return MOE_OK;
 }
 
