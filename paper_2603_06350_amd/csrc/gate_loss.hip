@@ -5,107 +5,227 @@
 //   moe_gate_distill    the mean over tokens of KL(softmax(target) || p), and its gradient
 // All three stream tables of T x E floats once: HBM-bound for large batches, launch-bound for small ones.
 //
-// One wave per token; lane l holds the scores of experts l, l + 64, ...  Sums over tokens stay in registers (a lane
-// keeps its experts), meet in LDS at the end of the block and go to the workspace as one row per block; a single
-// block then adds the rows in 64 bits, in a fixed order.
+// G lanes share a token, the least power of two with 4 G >= E; a lane holds four scores: consecutive ones in one load if
+// E is a multiple of 4 (VEC), those of experts l, l + G, ... otherwise.  So a wave reads 64 / G neighbouring rows at a
+// time, 1 KiB in one piece, whatever E is, and the sums over a row take log2(G) steps between lanes.
+//
+// Powers are taken of 2: with m the row's maximum and c = log2(e), e^(s-m) = 2^(c s - c m) is one fused multiply-add
+// (rounded once) and one v_exp_f32.  The rounding of c m is the same for a whole row and divides out of p.
+#include <type_traits>
+
 #include "moe_internal.h"
 
 namespace moe {
 
-constexpr int GL_THREADS = 256;
+constexpr int GL_THREADS = 512;
 constexpr int GL_WAVES = GL_THREADS / MOE_WAVE;
-constexpr int GL_BLOCKS = 512;        // most blocks of a launch that leaves partial sums
-constexpr int GL_FINISH = 1024;       // threads of the block that adds them
+constexpr int GL_FINISH = 1024;       // threads of the block that adds the blocks' sums
+constexpr float GL_LOG2E = 1.44269504088896340736f;
+constexpr float GL_LN2 = 0.693147180559945309417f;
 
-__device__ __forceinline__ float gl_wave_sum(float v) {
+// Sum and maximum over the G lanes of a token, on each of them: DPP steps inside a row of 16 lanes (xor 1, xor 2, then
+// the mirrors of 8 and of 16, as the lanes that they join hold equal values by then), exchanges beyond.
+template <int CTRL> __device__ __forceinline__ float gl_dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+template <int G, class Op> __device__ __forceinline__ float gl_reduce(float v, Op op) {
+  if constexpr (G >= 2) v = op(v, gl_dpp<0xB1>(v));      // quad_perm [1,0,3,2]
+  if constexpr (G >= 4) v = op(v, gl_dpp<0x4E>(v));      // quad_perm [2,3,0,1]
+  if constexpr (G >= 8) v = op(v, gl_dpp<0x141>(v));     // row_half_mirror
+  if constexpr (G >= 16) v = op(v, gl_dpp<0x140>(v));    // row_mirror
+  if constexpr (G >= 32) v = op(v, __shfl_xor(v, 16));
+  if constexpr (G >= 64) v = op(v, __shfl_xor(v, 32));
+  return v;
+}
+template <int G> __device__ __forceinline__ float gl_sum(float v) {
+  return gl_reduce<G>(v, [](float a, float b) { return a + b; });
+}
+template <int G> __device__ __forceinline__ float gl_max(float v) {
+  return gl_reduce<G>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The expert of value j of lane l of a token.
+template <int G, bool VEC> __device__ __forceinline__ int gl_expert(int l, int j) { return VEC ? 4 * l + j : l + G * j; }
+
+// A lane's four values of a row of a table, `fill` past the last expert.
+template <int G, bool VEC>
+__device__ __forceinline__ void gl_load(const float* __restrict__ row, int E, int l, float fill, float (&v)[4]) {
+  if constexpr (VEC) {
+    float4 q = make_float4(fill, fill, fill, fill);
+    if (4 * l < E) q = *reinterpret_cast<const float4*>(row + 4 * l);
+    v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int e = l + G * j;
+      v[j] = e < E ? row[e] : fill;
+    }
+  }
+}
+
+template <int G, bool VEC>
+__device__ __forceinline__ void gl_store(float* __restrict__ row, int E, int l, int accumulate, const float (&v)[4]) {
+  if constexpr (VEC) {
+    if (4 * l < E) {
+      float4* o = reinterpret_cast<float4*>(row + 4 * l);
+      float4 q = make_float4(v[0], v[1], v[2], v[3]);
+      if (accumulate) {
+        const float4 old = *o;
+        q = make_float4(q.x + old.x, q.y + old.y, q.z + old.z, q.w + old.w);
+      }
+      *o = q;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int e = l + G * j;
+      if (e < E) row[e] = accumulate ? row[e] + v[j] : v[j];
+    }
+  }
+}
+
+// c (s - m) of a row with the maximum m.  Where c m could pass the largest number (scores of the type's lowest value) m is
+// subtracted first; -inf: every s is, and the results are not used.
+struct GlBase {
+  float shift, scaled;
+  __device__ __forceinline__ explicit GlBase(float m) {
+    const bool far = fabsf(m) > 1e30f;
+    shift = far && m > -INFINITY ? m : 0.f;
+    scaled = far ? 0.f : GL_LOG2E * m;
+  }
+  __device__ __forceinline__ float exponent(float s) const { return fmaf(GL_LOG2E, s - shift, -scaled); }
+};
+
+// p = softmax of a row, zeros where every score is -inf.  log2p: its logarithms (of base 2).  Returns whether anything
+// is left of the row.
+template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4], float (&p)[4], float (*log2p)[4] = nullptr) {
+  const float m = gl_max<G>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+  const bool some = m > -INFINITY;
+  const GlBase base(m);
+  float t[4], sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    t[j] = base.exponent(s[j]);
+    p[j] = __builtin_amdgcn_exp2f(t[j]);
+    sum += p[j];
+  }
+  sum = gl_sum<G>(sum);
+  const float inv = some ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) p[j] *= inv;
+  if (log2p) {
+    const float log2sum = __builtin_amdgcn_logf(some ? sum : 1.f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) (*log2p)[j] = t[j] - log2sum;
+  }
+  return some;
+}
+
+// Sum over the block of one value per thread, in a fixed order, on every thread.  lds: one value per wave.
+template <class V> __device__ __forceinline__ V gl_block_sum(V v, V* lds) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-  return v;
-}
-__device__ __forceinline__ float gl_wave_max(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+  __syncthreads();
+  if (lane_id() == 0) lds[threadIdx.x / MOE_WAVE] = v;
+  __syncthreads();
+  v = 0;
+  for (int w = 0; w < static_cast<int>(blockDim.x / MOE_WAVE); ++w) v += lds[w];
   return v;
 }
 
-// The scores of token t, -inf past the last expert.
-template <int QE>
-__device__ __forceinline__ void gl_load(const float* __restrict__ scores, int64_t t, int E, int lane, float (&s)[QE]) {
+// The rows of a block, in turns of its waves, U batches of 64 / G rows at a time: load(data, row) of all of them, then
+// use(data, row, whether there is such a row, whether it counts) of each.
+template <int G, int U, class Data, class Load, class Use>
+__device__ __forceinline__ void gl_rows(int T, int per_block, const uint8_t* __restrict__ mask, Load load, Use use) {
+  constexpr int ROWS = MOE_WAVE / G;
+  const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
+  const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
+  for (int64_t t0 = begin + threadIdx.x / MOE_WAVE * (ROWS * U); t0 < end; t0 += GL_WAVES * ROWS * U) {
+    Data data[U];
+    bool real[U];
 #pragma unroll
-  for (int q = 0; q < QE; ++q) {
-    const int e = lane + q * MOE_WAVE;
-    s[q] = e < E ? scores[t * E + e] : -INFINITY;
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * ROWS + lane_id() / G, row = min(t, end - 1);
+      load(data[u], row);
+      real[u] = t < end && (!mask || mask[row]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * ROWS + lane_id() / G;
+      use(data[u], min(t, end - 1), t < end, real[u]);
+    }
   }
 }
 
-// p = softmax(s), zeros where every score is -inf; returns log(sum_e exp(s_e)) (-inf there).
-template <int QE> __device__ __forceinline__ float gl_softmax(const float (&s)[QE], float (&p)[QE]) {
-  float m = s[0];
-#pragma unroll
-  for (int q = 1; q < QE; ++q) m = fmaxf(m, s[q]);
-  m = gl_wave_max(m);
-  const bool empty = m == -INFINITY;
-  if (empty) m = 0.f;
-  float sum = 0.f;
-#pragma unroll
-  for (int q = 0; q < QE; ++q) {
-    p[q] = expf(s[q] - m);
-    sum += p[q];
-  }
-  sum = fmaxf(gl_wave_sum(sum), 1e-30f);     // 1 or more unless all are zero
-#pragma unroll
-  for (int q = 0; q < QE; ++q) p[q] /= sum;
-  return empty ? -INFINITY : m + logf(sum);
+__device__ __forceinline__ float gl_balance_loss(double dot, double total, int E, int k) {
+  return total > 0.0 ? static_cast<float>(dot * E * k / (total * total)) : 0.f;
 }
 
-template <int QE>
-__global__ __launch_bounds__(GL_THREADS) void balance_kernel(const float* __restrict__ scores,
-                                                             const int32_t* __restrict__ topk_idx,
-                                                             const uint8_t* __restrict__ mask, int T, int E, int k,
-                                                             float* __restrict__ part_p, int32_t* __restrict__ part_c) {
+// Counts and sums of a block's rows.  A single block finishes by itself (part_p is then not used), others leave a row of
+// the workspace each.
+template <int G, bool VEC>
+__global__ __launch_bounds__(GL_THREADS) void balance_kernel(const float* __restrict__ scores, const int32_t* __restrict__ topk_idx,
+                                                             const uint8_t* __restrict__ mask, int T, int E, int k, int per_block,
+                                                             float* __restrict__ part_p, int32_t* __restrict__ part_c,
+                                                             int32_t* __restrict__ counts, float* __restrict__ prob_sum,
+                                                             float* __restrict__ loss) {
   __shared__ float sum_p[GL_WAVES][MOE_MAX_E];
   __shared__ int32_t cnt[MOE_MAX_E];
-  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE;
-  cnt[threadIdx.x] = 0;
+  __shared__ double sums[GL_WAVES];
+  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, l = lane % G;
+  if (threadIdx.x < MOE_MAX_E) cnt[threadIdx.x] = 0;
   __syncthreads();
-  float acc[QE];
-#pragma unroll
-  for (int q = 0; q < QE; ++q) acc[q] = 0.f;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * GL_WAVES + wave; t < T; t += static_cast<int64_t>(gridDim.x) * GL_WAVES) {
-    if (mask && !mask[t]) continue;
-    float s[QE], p[QE];
-    gl_load(scores, t, E, lane, s);
-    if (lane < k) {
-      const int e = topk_idx[t * k + lane];
-      if (static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(&cnt[e], 1);
-    }
-    gl_softmax(s, p);
-#pragma unroll
-    for (int q = 0; q < QE; ++q) acc[q] += p[q];
+  const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
+  const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
+  for (int64_t a = begin * k + threadIdx.x; a < end * k; a += GL_THREADS) {
+    const int e = topk_idx[a];
+    if ((!mask || mask[a / k]) && static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(&cnt[e], 1);
   }
+  float acc[4] = {};
+  struct Row {
+    float s[4];
+  };
+  gl_rows<G, 4, Row>(
+      T, per_block, mask, [&](Row& r, int64_t t) { gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s); },
+      [&](Row& r, int64_t, bool, bool real) {
+        float p[4];
+        gl_softmax<G>(r.s, p);
 #pragma unroll
-  for (int q = 0; q < QE; ++q) sum_p[wave][lane + q * MOE_WAVE] = acc[q];
+        for (int j = 0; j < 4; ++j) acc[j] += real ? p[j] : 0.f;
+      });
+#pragma unroll
+  for (int off = G; off < MOE_WAVE; off <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], off);
+  if (lane < G) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int e = gl_expert<G, VEC>(l, j);
+      if (e < E) sum_p[wave][e] = acc[j];
+    }
+  }
   __syncthreads();
   const int e = threadIdx.x;
+  float v = 0.f;
+  int32_t c = 0;
   if (e < E) {
-    float v = 0.f;
     for (int w = 0; w < GL_WAVES; ++w) v += sum_p[w][e];
-    part_p[static_cast<int64_t>(blockIdx.x) * E + e] = v;
-    part_c[static_cast<int64_t>(blockIdx.x) * E + e] = cnt[e];
+    c = cnt[e];
   }
-}
-
-// Sum over the block of one value per thread, in a fixed order; valid on thread 0.
-template <class V> __device__ __forceinline__ V gl_block_sum(V v, V* lds) {
-  lds[threadIdx.x] = v;
-  __syncthreads();
-  for (int half = blockDim.x / 2; half >= 1; half >>= 1) {
-    if (threadIdx.x < static_cast<unsigned>(half)) lds[threadIdx.x] += lds[threadIdx.x + half];
-    __syncthreads();
+  if (gridDim.x > 1) {
+    if (e < E) {
+      part_p[static_cast<int64_t>(blockIdx.x) * E + e] = v;
+      part_c[static_cast<int64_t>(blockIdx.x) * E + e] = c;
+    }
+    return;
   }
-  const V r = lds[0];
-  __syncthreads();
-  return r;
+  const double total = gl_block_sum(static_cast<double>(c), sums);
+  const double dot = gl_block_sum(static_cast<double>(c) * v, sums);
+  if (e < E) {
+    counts[e] = c;
+    prob_sum[e] = v;
+  }
+  if (threadIdx.x == 0) *loss = gl_balance_loss(dot, total, E, k);
 }
 
 __global__ __launch_bounds__(GL_FINISH) void balance_finish_kernel(const float* __restrict__ part_p,
@@ -113,200 +233,282 @@ __global__ __launch_bounds__(GL_FINISH) void balance_finish_kernel(const float* 
                                                                    int k, int32_t* __restrict__ counts,
                                                                    float* __restrict__ prob_sum, float* __restrict__ loss) {
   __shared__ double sp[GL_FINISH];
-  __shared__ double sc[GL_FINISH];
-  const int e = threadIdx.x & (MOE_MAX_E - 1), g = threadIdx.x / MOE_MAX_E;
-  double p = 0.0, c = 0.0;
+  __shared__ int32_t sc[GL_FINISH];
+  __shared__ double sums[GL_FINISH / MOE_WAVE];
+  // `lanes` threads for a row of experts, the rows dealt to `groups` of them, eight rows on their way at a time
+  int lanes = 1;
+  while (lanes < E) lanes <<= 1;
+  const int groups = GL_FINISH / lanes, e = threadIdx.x % lanes, g = threadIdx.x / lanes;
+  double p = 0.0;
+  int32_t c = 0;
   if (e < E)
-    for (int b = g; b < blocks; b += GL_FINISH / MOE_MAX_E) {
-      p += part_p[static_cast<int64_t>(b) * E + e];
-      c += part_c[static_cast<int64_t>(b) * E + e];
+    for (int b = g; b < blocks; b += 8 * groups) {
+      float vp[8];
+      int32_t vc[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t at = static_cast<int64_t>(b + u * groups) * E + e;
+        const bool there = b + u * groups < blocks;
+        vp[u] = there ? part_p[at] : 0.f;
+        vc[u] = there ? part_c[at] : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        p += vp[u];
+        c += vc[u];
+      }
     }
   sp[threadIdx.x] = p;
   sc[threadIdx.x] = c;
   __syncthreads();
-  if (g == 0) {
-    for (int i = 1; i < GL_FINISH / MOE_MAX_E; ++i) {
-      p += sp[i * MOE_MAX_E + e];
-      c += sc[i * MOE_MAX_E + e];
+  for (int half = groups / 2; half >= 1; half >>= 1) {
+    if (g < half) {
+      sp[threadIdx.x] += sp[threadIdx.x + half * lanes];
+      sc[threadIdx.x] += sc[threadIdx.x + half * lanes];
     }
-    if (e < E) {
-      counts[e] = static_cast<int32_t>(c);
-      prob_sum[e] = static_cast<float>(p);
-    }
+    __syncthreads();
   }
-  __syncthreads();
-  const double total = gl_block_sum(g == 0 ? c : 0.0, sc);
-  const double dot = gl_block_sum(g == 0 ? c * p : 0.0, sp);
-  if (threadIdx.x == 0) *loss = total > 0.0 ? static_cast<float>(dot * E * k / (total * total)) : 0.f;
+  const bool mine = g == 0 && e < E;
+  p = mine ? sp[e] : 0.0;
+  c = mine ? sc[e] : 0;
+  const double total = gl_block_sum(static_cast<double>(c), sums);
+  const double dot = gl_block_sum(c * p, sums);
+  if (mine) {
+    counts[e] = c;
+    prob_sum[e] = static_cast<float>(p);
+  }
+  if (threadIdx.x == 0) *loss = gl_balance_loss(dot, total, E, k);
 }
 
 // ds = gradient of sum_j d_topk_w[j] w_j (w: the routing weights of moe_route) + gradient of coef * L.
 //   renorm 0: w_j = p[i_j]:                 ds_e = p_e (g_e - sum_l p_l g_l),  g_e = sum of d_topk_w[j] with i_j = e
 //   renorm 1: w = softmax over the chosen:  ds[i_j] = w_j (d_topk_w[j] - sum_l w_l d_topk_w[l])
 //   balance:  b_e = coef E k c_e / (sum c)^2, ds_e = p_e (b_e - sum_l p_l b_l)
-template <int QE>
+template <int G, bool VEC>
 __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float* __restrict__ scores,
                                                                     const int32_t* __restrict__ topk_idx,
                                                                     const float* __restrict__ d_topk_w,
                                                                     const int32_t* __restrict__ counts, float coef,
                                                                     const uint8_t* __restrict__ mask, int T, int E, int k,
-                                                                    int renorm, int accumulate, float* __restrict__ d_scores) {
-  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE;
-  float b[QE];
-#pragma unroll
-  for (int q = 0; q < QE; ++q) b[q] = 0.f;
+                                                                    int renorm, int accumulate, int per_block,
+                                                                    float* __restrict__ d_scores) {
+  const int lane = lane_id(), l = lane % G;
+  float b[4] = {};
   if (counts) {
     int64_t total = 0;
-    for (int e = 0; e < E; ++e) total += counts[e];
+    for (int e = lane; e < E; e += MOE_WAVE) total += counts[e];
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
     const double c = total > 0 ? static_cast<double>(coef) * E * k / (static_cast<double>(total) * static_cast<double>(total)) : 0.0;
 #pragma unroll
-    for (int q = 0; q < QE; ++q) {
-      const int e = lane + q * MOE_WAVE;
-      if (e < E) b[q] = static_cast<float>(c * counts[e]);
+    for (int j = 0; j < 4; ++j) {
+      const int e = gl_expert<G, VEC>(l, j);
+      if (e < E) b[j] = static_cast<float>(c * counts[e]);
     }
   }
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * GL_WAVES + wave; t < T; t += static_cast<int64_t>(gridDim.x) * GL_WAVES) {
-    float d[QE];
+  const bool with_p = counts || !renorm;             // the softmax over all experts has a part in it
+  struct Row {
+    float s[4], d[4];
+    int e[4];
+  };
+  gl_rows<G, 2, Row>(
+      T, per_block, mask,
+      [&](Row& r, int64_t t) {
+        gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
+        if (!d_topk_w) return;
+        // choices l, l + G, ... of the token are on lane l: k <= E <= 4 G
 #pragma unroll
-    for (int q = 0; q < QE; ++q) d[q] = 0.f;
-    if (!mask || mask[t]) {
-      float s[QE], p[QE], g[QE], chosen[QE];
-      gl_load(scores, t, E, lane, s);
-      gl_softmax(s, p);
-#pragma unroll
-      for (int q = 0; q < QE; ++q) {
-        g[q] = b[q];
-        chosen[q] = 0.f;
-      }
-      if (d_topk_w) {
-        int my_e = lane < k ? topk_idx[t * k + lane] : -1;
-        if (static_cast<unsigned>(my_e) >= static_cast<unsigned>(E)) my_e = -1;
-        float my_d = my_e >= 0 ? d_topk_w[t * k + lane] : 0.f;
-        if (renorm) {
-          const float my_s = my_e >= 0 ? scores[t * E + my_e] : -INFINITY;
-          float m = gl_wave_max(my_s);
-          if (m == -INFINITY) m = 0.f;
-          float w = my_e >= 0 ? expf(my_s - m) : 0.f;
-          w /= fmaxf(gl_wave_sum(w), 1e-30f);
-          my_d = w * (my_d - gl_wave_sum(w * my_d));
+        for (int q = 0; q < 4; ++q) {
+          const int j = l + G * q;
+          r.e[q] = j < k ? topk_idx[t * k + j] : -1;
+          r.d[q] = j < k ? d_topk_w[t * k + j] : 0.f;
         }
-        for (int j = 0; j < k; ++j) {
-          const int e = __shfl(my_e, j);
-          const float v = __shfl(my_d, j);
+      },
+      [&](Row& r, int64_t t, bool there, bool real) {
+        float p[4] = {}, d[4] = {}, chosen[4] = {};
+        if (with_p) gl_softmax<G>(r.s, p);
+        if (d_topk_w) {
 #pragma unroll
-          for (int q = 0; q < QE; ++q)
-            if (e == lane + q * MOE_WAVE) (renorm ? chosen[q] : g[q]) += v;
+          for (int q = 0; q < 4; ++q)
+            if (static_cast<unsigned>(r.e[q]) >= static_cast<unsigned>(E)) r.e[q] = -1, r.d[q] = 0.f;
+          if (renorm) {
+            float w[4], m = -INFINITY, sum = 0.f, dot = 0.f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              w[q] = r.e[q] >= 0 ? scores[t * E + r.e[q]] : -INFINITY;
+              m = fmaxf(m, w[q]);
+            }
+            m = gl_max<G>(m);
+            const bool some = m > -INFINITY;
+            const GlBase base(m);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              w[q] = __builtin_amdgcn_exp2f(base.exponent(w[q]));
+              sum += w[q];
+            }
+            sum = gl_sum<G>(sum);
+            const float inv = some ? 1.f / sum : 0.f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              w[q] *= inv;
+              dot += w[q] * r.d[q];
+            }
+            dot = gl_sum<G>(dot);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) r.d[q] = w[q] * (r.d[q] - dot);
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int n = min(k - G * q, G);         // the same for all lanes
+            for (int i = 0; i < n; ++i) {
+              const int e = __shfl(r.e[q], (lane & ~(G - 1)) + i);
+              const float v = __shfl(r.d[q], (lane & ~(G - 1)) + i);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) chosen[j] += e == gl_expert<G, VEC>(l, j) ? v : 0.f;
+            }
+          }
         }
-      }
-      float dot = 0.f;
+        if (with_p) {
+          float g[4];
 #pragma unroll
-      for (int q = 0; q < QE; ++q) dot += p[q] * g[q];
-      dot = gl_wave_sum(dot);
+          for (int j = 0; j < 4; ++j) g[j] = renorm ? b[j] : b[j] + chosen[j];
+          const float dot = gl_sum<G>((p[0] * g[0] + p[1] * g[1]) + (p[2] * g[2] + p[3] * g[3]));
 #pragma unroll
-      for (int q = 0; q < QE; ++q) d[q] = p[q] * (g[q] - dot) + chosen[q];
-    }
+          for (int j = 0; j < 4; ++j) d[j] = p[j] * (g[j] - dot);
+        }
 #pragma unroll
-    for (int q = 0; q < QE; ++q) {
-      const int e = lane + q * MOE_WAVE;
-      if (e < E) d_scores[t * E + e] = accumulate ? d_scores[t * E + e] + d[q] : d[q];
-    }
-  }
+        for (int j = 0; j < 4; ++j) d[j] = real ? d[j] + (renorm ? chosen[j] : 0.f) : 0.f;
+        if (there && (real || !accumulate)) gl_store<G, VEC>(d_scores + t * E, E, l, accumulate, d);
+      });
 }
 
-// Tokens that the mask keeps, one number per block.
-__global__ __launch_bounds__(GL_THREADS) void mask_count_kernel(const uint8_t* __restrict__ mask, int T, int32_t* __restrict__ part) {
-  __shared__ int32_t lds[GL_THREADS];
+// Bytes of a mask that are not 0, over the block; the same on every thread.
+__device__ __forceinline__ int gl_count_mask(const uint8_t* __restrict__ mask, int64_t begin, int64_t end, int* lds) {
   int n = 0;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * GL_THREADS + threadIdx.x; t < T; t += static_cast<int64_t>(gridDim.x) * GL_THREADS)
-    n += mask[t] != 0;
-  n = gl_block_sum(n, lds);
+  auto word = [](uint32_t v) { return __popc(((v & 0x7F7F7F7Fu) + 0x7F7F7F7Fu | v) & 0x80808080u); };
+  int64_t first = begin + (-static_cast<int64_t>(reinterpret_cast<uintptr_t>(mask) + begin) & 15);
+  if (first > end) first = end;
+  const int64_t chunks = (end - first) / 16;
+  for (int64_t t = begin + threadIdx.x; t < first; t += blockDim.x) n += mask[t] != 0;
+  for (int64_t t = first + chunks * 16 + threadIdx.x; t < end; t += blockDim.x) n += mask[t] != 0;
+  for (int64_t i = threadIdx.x; i < chunks; i += blockDim.x) {
+    const uint4 v = *reinterpret_cast<const uint4*>(mask + first + i * 16);
+    n += word(v.x) + word(v.y) + word(v.z) + word(v.w);
+  }
+  return gl_block_sum(n, lds);
+}
+
+constexpr int GL_COUNT_BLOCKS = 64;
+__global__ __launch_bounds__(GL_THREADS) void mask_count_kernel(const uint8_t* __restrict__ mask, int T, int32_t* __restrict__ part) {
+  __shared__ int lds[GL_WAVES];
+  const int64_t per = (static_cast<int64_t>(T) + GL_COUNT_BLOCKS - 1) / GL_COUNT_BLOCKS;
+  const int64_t begin = min(blockIdx.x * per, static_cast<int64_t>(T));
+  const int n = gl_count_mask(mask, begin, min(begin + per, static_cast<int64_t>(T)), lds);
   if (threadIdx.x == 0) part[blockIdx.x] = n;
 }
 
-// Tokens that count, from the blocks of mask_count_kernel (T without a mask); the same on every thread.
-__device__ __forceinline__ double gl_tokens(const int32_t* __restrict__ part_n, int n_blocks, int T) {
-  if (!part_n) return T;
-  double n = 0.0;
-  for (int b = 0; b < n_blocks; ++b) n += part_n[b];
+// Tokens that count: T without a mask; from mask_count_kernel's parts; or counted by the block.
+__device__ __forceinline__ double gl_tokens(const uint8_t* __restrict__ mask, const int32_t* __restrict__ part_n, int T, int* lds) {
+  if (!mask) return T;
+  if (!part_n) return gl_count_mask(mask, 0, T, lds);
+  int n = part_n[lane_id()];
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off);
   return n;
 }
+static_assert(GL_COUNT_BLOCKS == MOE_WAVE, "one part per lane");
 
-template <int QE>
-__global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __restrict__ scores,
-                                                             const float* __restrict__ target,
-                                                             const uint8_t* __restrict__ mask,
-                                                             const int32_t* __restrict__ part_n, int n_blocks, int T, int E,
-                                                             float coef, int accumulate, double* __restrict__ part_loss,
+template <int G, bool VEC>
+__global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __restrict__ scores, const float* __restrict__ target,
+                                                             const uint8_t* __restrict__ mask, const int32_t* __restrict__ part_n,
+                                                             int T, int E, float coef, int accumulate, int per_block,
+                                                             double* __restrict__ part_loss, float* __restrict__ loss,
                                                              float* __restrict__ d_scores) {
-  __shared__ double lds[GL_THREADS];
-  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE;
-  const double n = gl_tokens(part_n, n_blocks, T);
+  __shared__ double lds[GL_WAVES];
+  __shared__ int lds_n[GL_WAVES];
+  const int lane = lane_id(), l = lane % G;
+  const double n = gl_tokens(mask, part_n, T, lds_n);
   const float scale = n > 0.0 ? static_cast<float>(coef / n) : 0.f;
-  double loss = 0.0;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * GL_WAVES + wave; t < T; t += static_cast<int64_t>(gridDim.x) * GL_WAVES) {
-    float d[QE];
-#pragma unroll
-    for (int q = 0; q < QE; ++q) d[q] = 0.f;
-    if (!mask || mask[t]) {
-      float s[QE], u[QE], p[QE], w[QE];
-      gl_load(scores, t, E, lane, s);
-      gl_load(target, t, E, lane, u);
-      const float lp = gl_softmax(s, p), lq = gl_softmax(u, w);
-      if (lp > -INFINITY && lq > -INFINITY) {
+  double sum = 0.0;
+  struct Row {
+    float s[4], u[4];
+  };
+  gl_rows<G, 2, Row>(
+      T, per_block, mask,
+      [&](Row& r, int64_t t) {
+        gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
+        gl_load<G, VEC>(target + t * E, E, l, -INFINITY, r.u);
+      },
+      [&](Row& r, int64_t t, bool there, bool real) {
+        float p[4], q[4], lp[4], lq[4], d[4];
+        const bool left_p = gl_softmax<G>(r.s, p, &lp), left_q = gl_softmax<G>(r.u, q, &lq);
+        const bool counts = real && left_p && left_q;
         float row = 0.f;
 #pragma unroll
-        for (int q = 0; q < QE; ++q) {
-          const int e = lane + q * MOE_WAVE;
-          if (e < E && w[q] > 0.f) row += w[q] * ((u[q] - lq) - (s[q] - lp));
-          d[q] = scale * (p[q] - w[q]);
+        for (int j = 0; j < 4; ++j) {
+          row += q[j] > 0.f ? q[j] * (lq[j] - lp[j]) : 0.f;      // q = 0 has no part
+          d[j] = counts ? scale * (p[j] - q[j]) : 0.f;
         }
-        loss += row;
-      }
-    }
-    if (d_scores) {
-#pragma unroll
-      for (int q = 0; q < QE; ++q) {
-        const int e = lane + q * MOE_WAVE;
-        if (e < E) d_scores[t * E + e] = accumulate ? d_scores[t * E + e] + d[q] : d[q];
-      }
-    }
-  }
-  loss = gl_block_sum(loss, lds);
-  if (threadIdx.x == 0) part_loss[blockIdx.x] = loss;
+        sum += counts ? row : 0.f;
+        if (d_scores && there && (real || !accumulate)) gl_store<G, VEC>(d_scores + t * E, E, l, accumulate, d);
+      });
+  sum = gl_block_sum(sum * GL_LN2, lds);
+  if (threadIdx.x != 0) return;
+  if (gridDim.x > 1)
+    part_loss[blockIdx.x] = sum;
+  else
+    *loss = n > 0.0 ? static_cast<float>(sum / n) : 0.f;
 }
 
+// The mean of the blocks' losses.  (T == 0: no blocks, and 0.)
 __global__ __launch_bounds__(GL_FINISH) void distill_finish_kernel(const double* __restrict__ part_loss, int blocks,
-                                                                   const int32_t* __restrict__ part_n, int n_blocks, int T,
-                                                                   float* __restrict__ loss) {
-  __shared__ double lds[GL_FINISH];
+                                                                   const uint8_t* __restrict__ mask, const int32_t* __restrict__ part_n,
+                                                                   int T, float* __restrict__ loss) {
+  __shared__ double lds[GL_FINISH / MOE_WAVE];
+  __shared__ int lds_n[GL_FINISH / MOE_WAVE];
+  const double n = gl_tokens(mask, part_n, T, lds_n);
   const double sum = gl_block_sum(static_cast<int>(threadIdx.x) < blocks ? part_loss[threadIdx.x] : 0.0, lds);
-  const double n = gl_tokens(part_n, n_blocks, T);
   if (threadIdx.x == 0) *loss = n > 0.0 ? static_cast<float>(sum / n) : 0.f;
 }
 
-static_assert(GL_BLOCKS <= GL_FINISH, "one partial loss per thread");
-
-static int gl_blocks(int T) {
-  const int64_t b = (static_cast<int64_t>(T) + GL_WAVES - 1) / GL_WAVES;
-  return static_cast<int>(b < GL_BLOCKS ? b : GL_BLOCKS);
+// Calls f with the lanes per token and whether rows are whole 16-byte chunks.
+template <class F> static void gl_by_experts(int E, F f) {
+  auto with = [&](auto g) {
+    if (E % 4 == 0)
+      f(g, std::true_type{});
+    else
+      f(g, std::false_type{});
+  };
+  if (E <= 4) with(std::integral_constant<int, 1>{});
+  else if (E <= 8) with(std::integral_constant<int, 2>{});
+  else if (E <= 16) with(std::integral_constant<int, 4>{});
+  else if (E <= 32) with(std::integral_constant<int, 8>{});
+  else if (E <= 64) with(std::integral_constant<int, 16>{});
+  else if (E <= 128) with(std::integral_constant<int, 32>{});
+  else with(std::integral_constant<int, 64>{});
 }
-constexpr int GL_COUNT_BLOCKS = 64;
 
-// Kernel variant by the number of scores per lane.
-#define GL_BY_E(E, CALL) \
-  do {                   \
-    if ((E) <= 64) {     \
-      constexpr int QE = 1; CALL; \
-    } else if ((E) <= 128) { \
-      constexpr int QE = 2; CALL; \
-    } else {             \
-      constexpr int QE = 4; CALL; \
-    }                    \
-  } while (0)
+// Blocks and rows of each.  A block that leaves partial sums takes 32 KiB of scores or more, and there are 256 of them at
+// most, as one block adds them up; what needs no sums takes 16 KiB and up to 2048 blocks.
+struct GlPlan {
+  int blocks, per_block;
+};
+static GlPlan gl_plan(int T, int E, bool sums) {
+  const int64_t least = (sums ? 8192 : 4096) / E + 1, most_blocks = sums ? 256 : 2048;
+  int64_t per = (static_cast<int64_t>(T) + most_blocks - 1) / most_blocks;
+  if (per < least) per = least;
+  const int rows = GL_WAVES * 64 / (E <= 4 ? 1 : E <= 8 ? 2 : E <= 16 ? 4 : E <= 32 ? 8 : E <= 64 ? 16 : E <= 128 ? 32 : 64);
+  per = (per + rows - 1) / rows * rows;
+  if (per > T) per = T;
+  return {T > 0 ? static_cast<int>((T + per - 1) / per) : 0, static_cast<int>(per)};
+}
+
+// From this many tokens on the mask is counted by a launch of its own, not by every block.
+constexpr int GL_COUNT_FROM = 1 << 14;
 
 size_t gate_loss_workspace_bytes(const moe_shape_t* shape) {
-  const size_t b = static_cast<size_t>(gl_blocks(shape->T));
-  const size_t balance = b * shape->E * 8, distill = b * 8 + GL_COUNT_BLOCKS * 4;
+  const size_t b = static_cast<size_t>(gl_plan(shape->T, shape->E, true).blocks);
+  const size_t balance = b > 1 ? b * shape->E * 8 : 0, distill = b * 8 + GL_COUNT_BLOCKS * 4;
   return balance > distill ? balance : distill;
 }
 
@@ -323,14 +525,17 @@ extern "C" int moe_balance_loss(const moe_shape_t* shape, const float* scores, c
   if (shape->T > 0 && (!scores || !topk_idx || !aligned16(scores))) return MOE_ERR_INVALID_ARG;
   if (workspace_bytes < gate_loss_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const int T = shape->T, E = shape->E, k = shape->k, blocks = gl_blocks(T);
+  const int T = shape->T, E = shape->E, k = shape->k;
+  const GlPlan plan = gl_plan(T, E, true);
   float* part_p = static_cast<float*>(workspace);
-  int32_t* part_c = reinterpret_cast<int32_t*>(part_p + static_cast<size_t>(blocks) * E);
-  if (blocks > 0)
-    GL_BY_E(E, hipLaunchKernelGGL((balance_kernel<QE>), dim3(blocks), dim3(GL_THREADS), 0, st, scores, topk_idx,
-                                  token_mask, T, E, k, part_p, part_c));
-  hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(GL_FINISH), 0, st, part_p, part_c, blocks, E, k, counts,
-                     prob_sum, loss);
+  int32_t* part_c = reinterpret_cast<int32_t*>(part_p + static_cast<size_t>(plan.blocks) * E);
+  if (T > 0)
+    gl_by_experts(E, [&](auto g, auto vec) {
+      hipLaunchKernelGGL((balance_kernel<g(), vec()>), dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, topk_idx, token_mask, T, E, k,
+                         plan.per_block, part_p, part_c, counts, prob_sum, loss);
+    });
+  if (plan.blocks != 1)
+    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(GL_FINISH), 0, st, part_p, part_c, plan.blocks, E, k, counts, prob_sum, loss);
   return launch_status();
 }
 
@@ -348,8 +553,11 @@ extern "C" int moe_route_backward(const moe_shape_t* shape, const float* scores,
     return MOE_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E, k = shape->k;
-  GL_BY_E(E, hipLaunchKernelGGL((route_backward_kernel<QE>), dim3(gl_blocks(T)), dim3(GL_THREADS), 0, st, scores, topk_idx,
-                                d_topk_w, counts, balance_coef, token_mask, T, E, k, shape->renorm, accumulate, d_scores));
+  const GlPlan plan = gl_plan(T, E, false);
+  gl_by_experts(E, [&](auto g, auto vec) {
+    hipLaunchKernelGGL((route_backward_kernel<g(), vec()>), dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, topk_idx, d_topk_w, counts,
+                       balance_coef, token_mask, T, E, k, shape->renorm, accumulate, plan.per_block, d_scores);
+  });
   return launch_status();
 }
 
@@ -365,15 +573,20 @@ extern "C" int moe_gate_distill(const moe_shape_t* shape, const float* scores, c
   if (!aligned16(d_scores) || !aligned4(loss)) return MOE_ERR_INVALID_ARG;
   if (workspace_bytes < gate_loss_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const int T = shape->T, E = shape->E, blocks = gl_blocks(T);
+  const int T = shape->T, E = shape->E;
+  const GlPlan plan = gl_plan(T, E, true);
   double* part_loss = static_cast<double*>(workspace);
-  int32_t* part_n = token_mask ? reinterpret_cast<int32_t*>(part_loss + blocks) : nullptr;
-  if (token_mask && T > 0)
+  int32_t* part_n = nullptr;
+  if (token_mask && T >= GL_COUNT_FROM) {
+    part_n = reinterpret_cast<int32_t*>(part_loss + plan.blocks);
     hipLaunchKernelGGL(mask_count_kernel, dim3(GL_COUNT_BLOCKS), dim3(GL_THREADS), 0, st, token_mask, T, part_n);
-  if (blocks > 0)
-    GL_BY_E(E, hipLaunchKernelGGL((distill_kernel<QE>), dim3(blocks), dim3(GL_THREADS), 0, st, scores, target_scores,
-                                  token_mask, part_n, GL_COUNT_BLOCKS, T, E, coef, accumulate, part_loss, d_scores));
-  hipLaunchKernelGGL(distill_finish_kernel, dim3(1), dim3(GL_FINISH), 0, st, part_loss, blocks, T > 0 ? part_n : nullptr,
-                     GL_COUNT_BLOCKS, T, loss);
+  }
+  if (T > 0)
+    gl_by_experts(E, [&](auto g, auto vec) {
+      hipLaunchKernelGGL((distill_kernel<g(), vec()>), dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, target_scores, token_mask, part_n, T,
+                         E, coef, accumulate, plan.per_block, part_loss, loss, d_scores);
+    });
+  if (plan.blocks != 1)
+    hipLaunchKernelGGL(distill_finish_kernel, dim3(1), dim3(GL_FINISH), 0, st, part_loss, plan.blocks, token_mask, part_n, T, loss);
   return launch_status();
 }

@@ -12,8 +12,8 @@ namespace moe {
 
 constexpr int GR_THREADS = 256;
 constexpr int GR_TENSORS = 128;        // tensors of one launch
-constexpr int64_t GR_PIECE = 4096;     // least elements of a piece; all pieces of a call have the same size
-constexpr int64_t GR_PIECES = 2048;    // pieces of a call that is large enough
+constexpr int64_t GR_PIECE = 8192;     // least elements of a piece; all pieces of a call have the same size
+constexpr int64_t GR_PIECES = 4096;    // pieces of a call that is large enough
 
 struct GradTable {
   const void* data[GR_TENSORS];
@@ -151,15 +151,18 @@ template <bool BF16> __device__ __forceinline__ void grad_scale(const GradPiece&
 }
 
 // Every block makes the factor from the pieces' sums by itself, which saves a launch.  The pieces are taken from the last
-// to the first: those that the norm's pass read last are in the memory-side cache.
-__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, int count, int64_t piece, const double* __restrict__ part,
+// eight to the first: what the norm's pass read last is in the memory-side cache, and in the L2 of the XCD that block b
+// of both passes runs on (b % 8).  The grid is a multiple of 8.
+__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, int count, int blocks, int64_t piece, const double* __restrict__ part,
                                                                 int64_t pieces, double max_norm, float* __restrict__ norm) {
   __shared__ double lds[GR_THREADS / MOE_WAVE];
   const double s = grad_total_norm(part, pieces, lds);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(s);
   // 1 where the norm is no finite number: the caller sees it in `norm`
   const float c = s > max_norm && s < INFINITY ? static_cast<float>(max_norm / s) : 1.f;
-  const GradPiece g = grad_piece(tab, count, piece, gridDim.x - 1 - blockIdx.x);
+  const int b = (gridDim.x / 8 - 1 - blockIdx.x / 8) * 8 + blockIdx.x % 8;
+  if (b >= blocks) return;
+  const GradPiece g = grad_piece(tab, count, piece, b);
   if (c == 1.f && g.out == g.data) return;
   if (g.bf16)
     grad_scale<true>(g, c);
@@ -234,7 +237,7 @@ static int grads_call(int32_t count, const moe_tensor_t* tensors, bool clip, dou
   });
   if (clip && pieces > 0)
     for_tables(count, tensors, piece, [&](const GradTable& tab, int n, int blocks) {
-      hipLaunchKernelGGL(grad_scale_kernel, dim3(blocks), dim3(GR_THREADS), 0, st, tab, n, piece, part, pieces, max_norm, norm);
+      hipLaunchKernelGGL(grad_scale_kernel, dim3((blocks + 7) / 8 * 8), dim3(GR_THREADS), 0, st, tab, n, blocks, piece, part, pieces, max_norm, norm);
     });
   else
     hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(GR_THREADS), 0, st, part, pieces, norm);
