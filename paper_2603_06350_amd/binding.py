@@ -253,14 +253,15 @@ def moe_place_replicas(E, loads, replicas, n_gpus, prev_replicas, prev_gpu, gpu_
 # ---- training a gate.  Tensors given to these calls are checked here (type, size, contiguity, the current GPU), as a
 # ---- mask or a gradient of another size would be read out of range; plain device addresses (int) are taken as they are.
 _F32, _I32, _MASK, _BYTES = "f32", "i32", "mask", "bytes"
-_types = None
+_types = _current_gpu = None
 
 
 def _tensor_types():
     """The torch types of each kind of argument; the kinds MOE_F32 and MOE_BF16 are storage in a shape's dtype."""
-    global _types
+    global _types, _current_gpu
     if _types is None:
         import torch
+        _current_gpu = torch.cuda.current_device
         _types = {_F32: (torch.float32,), _I32: (torch.int32,), _MASK: (torch.bool, torch.uint8),
                   _BYTES: (torch.uint8, torch.int8), MOE_F32: (torch.float32,), MOE_BF16: (torch.bfloat16,)}
     return _types
@@ -269,21 +270,23 @@ def _tensor_types():
 def _addresses(call, *operands):
     """Device addresses of (name, tensor or address or None, kind, elements) operands, after their checks.  A buffer of
     bytes may be larger than asked for."""
-    out, gpu = [], None
+    out, gpu, types = [], None, None
     for name, t, kind, numel in operands:
-        if t is None or isinstance(t, int):
+        if t is None or type(t) is int:
             out.append(t)
             continue
-        if gpu is None and t.is_cuda:
-            import torch
-            gpu = torch.cuda.current_device()
-        types = _tensor_types()[kind]
+        if types is None:
+            types = _tensor_types()
+            if t.is_cuda:
+                gpu = _current_gpu()
         have = t.numel()
-        if t.get_device() != gpu or t.dtype not in types or not t.is_contiguous() or \
-                (have < numel if kind is _BYTES else have != numel):
-            raise ValueError(f"{call}: {name} has to be a contiguous tensor of {numel} x {' or '.join(map(str, types))} "
-                             f"on the current GPU, not {list(t.shape)} of {t.dtype}, strides {list(t.stride())}, on {t.device}")
-        out.append(t.data_ptr())
+        if t.get_device() == gpu and t.dtype in types[kind] and t.is_contiguous() and \
+                (have == numel or have > numel and kind is _BYTES):
+            out.append(t.data_ptr())
+            continue
+        want = " or ".join(map(str, types[kind]))
+        raise ValueError(f"{call}: {name} has to be a contiguous tensor of {numel} x {want} on the current GPU, not "
+                         f"{list(t.shape)} of {t.dtype}, strides {list(t.stride())}, on {t.device}")
     return out
 
 

@@ -17,9 +17,8 @@
 
 namespace moe {
 
-constexpr int GL_THREADS = 512;
-constexpr int GL_WAVES = GL_THREADS / MOE_WAVE;
-constexpr int GL_FINISH = 1024;       // threads of the block that adds the blocks' sums
+constexpr int GL_SUM_THREADS = 1024;  // of a block that leaves a row of sums, and of the block that adds these rows
+constexpr int GL_THREADS = 256;       // of the others
 constexpr float GL_LOG2E = 1.44269504088896340736f;
 constexpr float GL_LN2 = 0.693147180559945309417f;
 
@@ -47,39 +46,32 @@ template <int G> __device__ __forceinline__ float gl_max(float v) {
 // The expert of value j of lane l of a token.
 template <int G, bool VEC> __device__ __forceinline__ int gl_expert(int l, int j) { return VEC ? 4 * l + j : l + G * j; }
 
-// A lane's four values of a row of a table, `fill` past the last expert.
+// A lane's four values of a row of a table, `fill` past the last expert.  (No load is behind a branch: lanes past the end
+// read the last values again.  The compiler counts on no load that a branch may skip, and would wait for all of them.)
 template <int G, bool VEC>
 __device__ __forceinline__ void gl_load(const float* __restrict__ row, int E, int l, float fill, float (&v)[4]) {
   if constexpr (VEC) {
-    float4 q = make_float4(fill, fill, fill, fill);
-    if (4 * l < E) q = *reinterpret_cast<const float4*>(row + 4 * l);
-    v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+    const float4 q = *reinterpret_cast<const float4*>(row + min(4 * l, E - 4));
+    const bool there = 4 * l < E;
+    v[0] = there ? q.x : fill, v[1] = there ? q.y : fill, v[2] = there ? q.z : fill, v[3] = there ? q.w : fill;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int e = l + G * j;
-      v[j] = e < E ? row[e] : fill;
+      v[j] = row[min(e, E - 1)];
+      v[j] = e < E ? v[j] : fill;
     }
   }
 }
 
-template <int G, bool VEC>
-__device__ __forceinline__ void gl_store(float* __restrict__ row, int E, int l, int accumulate, const float (&v)[4]) {
+template <int G, bool VEC> __device__ __forceinline__ void gl_store(float* __restrict__ row, int E, int l, const float (&v)[4]) {
   if constexpr (VEC) {
-    if (4 * l < E) {
-      float4* o = reinterpret_cast<float4*>(row + 4 * l);
-      float4 q = make_float4(v[0], v[1], v[2], v[3]);
-      if (accumulate) {
-        const float4 old = *o;
-        q = make_float4(q.x + old.x, q.y + old.y, q.z + old.z, q.w + old.w);
-      }
-      *o = q;
-    }
+    if (4 * l < E) *reinterpret_cast<float4*>(row + 4 * l) = make_float4(v[0], v[1], v[2], v[3]);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int e = l + G * j;
-      if (e < E) row[e] = accumulate ? row[e] + v[j] : v[j];
+      if (e < E) row[e] = v[j];
     }
   }
 }
@@ -133,29 +125,49 @@ template <class V> __device__ __forceinline__ V gl_block_sum(V v, V* lds) {
   return v;
 }
 
-// The rows of a block, in turns of its waves, U batches of 64 / G rows at a time: load(data, row) of all of them, then
-// use(data, row, whether there is such a row, whether it counts) of each.
-template <int G, int U, class Data, class Load, class Use>
-__device__ __forceinline__ void gl_rows(int T, int per_block, const uint8_t* __restrict__ mask, Load load, Use use) {
+// The rows of a block (which has one or more), in turns of its waves, U batches of 64 / G rows at a time: load(data, row) of
+// all of them, then use(data, row, whether there is such a row, whether it counts) of each.  The loads of a turn are on
+// their way during the turn before, those of the first during `first`; past the end the last row is read again.
+// `table`: T bytes or more, read where there is no mask.
+template <int G, int U, class Data, class Load, class First, class Use>
+__device__ __forceinline__ void gl_rows(int T, int per_block, const uint8_t* __restrict__ mask, const void* table, Load load, First first,
+                                        Use use) {
   constexpr int ROWS = MOE_WAVE / G;
   const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
   const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
-  for (int64_t t0 = begin + threadIdx.x / MOE_WAVE * (ROWS * U); t0 < end; t0 += GL_WAVES * ROWS * U) {
+  struct Turn {
     Data data[U];
-    bool real[U];
+    uint8_t mask[U];
+  };
+  const uint8_t* some_bytes = mask ? mask : static_cast<const uint8_t*>(table);
+  auto start = [&](Turn& n, int64_t t0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * ROWS + lane_id() / G, row = min(t, end - 1);
-      load(data[u], row);
-      real[u] = t < end && (!mask || mask[row]);
+      const int64_t row = min(t0 + u * ROWS + lane_id() / G, end - 1);
+      n.mask[u] = some_bytes[row];
+      load(n.data[u], row);
     }
+  };
+  const int64_t step = blockDim.x / MOE_WAVE * (ROWS * U);
+  int64_t t0 = begin + threadIdx.x / MOE_WAVE * (ROWS * U);
+  Turn now;
+  start(now, t0);
+  first();
+  while (t0 < end) {
+    Turn next;
+    start(next, t0 + step);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t t = t0 + u * ROWS + lane_id() / G;
-      use(data[u], min(t, end - 1), t < end, real[u]);
+      use(now.data[u], min(t, end - 1), t < end, t < end && (!mask || now.mask[u]));
     }
+    now = next;
+    t0 += step;
   }
 }
+
+// A block's row of sums in the workspace, whole 16-byte chunks.
+constexpr int gl_part_pitch(int E) { return (E + 3) / 4 * 4; }
 
 __device__ __forceinline__ float gl_balance_loss(double dot, double total, int E, int k) {
   return total > 0.0 ? static_cast<float>(dot * E * k / (total * total)) : 0.f;
@@ -164,29 +176,32 @@ __device__ __forceinline__ float gl_balance_loss(double dot, double total, int E
 // Counts and sums of a block's rows.  A single block finishes by itself (part_p is then not used), others leave a row of
 // the workspace each.
 template <int G, bool VEC>
-__global__ __launch_bounds__(GL_THREADS) void balance_kernel(const float* __restrict__ scores, const int32_t* __restrict__ topk_idx,
+__global__ __launch_bounds__(GL_SUM_THREADS) void balance_kernel(const float* __restrict__ scores, const int32_t* __restrict__ topk_idx,
                                                              const uint8_t* __restrict__ mask, int T, int E, int k, int per_block,
                                                              float* __restrict__ part_p, int32_t* __restrict__ part_c,
                                                              int32_t* __restrict__ counts, float* __restrict__ prob_sum,
                                                              float* __restrict__ loss) {
-  __shared__ float sum_p[GL_WAVES][MOE_MAX_E];
+  constexpr int WAVES = GL_SUM_THREADS / MOE_WAVE;
+  __shared__ float sum_p[WAVES][MOE_MAX_E];
   __shared__ int32_t cnt[MOE_MAX_E];
-  __shared__ double sums[GL_WAVES];
+  __shared__ double sums[WAVES];
   const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, l = lane % G;
   if (threadIdx.x < MOE_MAX_E) cnt[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
-  const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
-  for (int64_t a = begin * k + threadIdx.x; a < end * k; a += GL_THREADS) {
-    const int e = topk_idx[a];
-    if ((!mask || mask[a / k]) && static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(&cnt[e], 1);
-  }
   float acc[4] = {};
   struct Row {
     float s[4];
   };
-  gl_rows<G, 4, Row>(
-      T, per_block, mask, [&](Row& r, int64_t t) { gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s); },
+  gl_rows<G, 2, Row>(
+      T, per_block, mask, scores, [&](Row& r, int64_t t) { gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s); },
+      [&] {
+        const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
+        const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
+        for (int64_t a = begin * k + threadIdx.x; a < end * k; a += GL_SUM_THREADS) {
+          const int e = topk_idx[a];
+          if ((!mask || mask[a / k]) && static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(&cnt[e], 1);
+        }
+      },
       [&](Row& r, int64_t, bool, bool real) {
         float p[4];
         gl_softmax<G>(r.s, p);
@@ -209,13 +224,14 @@ __global__ __launch_bounds__(GL_THREADS) void balance_kernel(const float* __rest
   float v = 0.f;
   int32_t c = 0;
   if (e < E) {
-    for (int w = 0; w < GL_WAVES; ++w) v += sum_p[w][e];
+    for (int w = 0; w < WAVES; ++w) v += sum_p[w][e];
     c = cnt[e];
   }
   if (gridDim.x > 1) {
-    if (e < E) {
-      part_p[static_cast<int64_t>(blockIdx.x) * E + e] = v;
-      part_c[static_cast<int64_t>(blockIdx.x) * E + e] = c;
+    const int pitch = gl_part_pitch(E);
+    if (e < pitch) {
+      part_p[blockIdx.x * pitch + e] = v;
+      part_c[blockIdx.x * pitch + e] = c;
     }
     return;
   }
@@ -228,54 +244,64 @@ __global__ __launch_bounds__(GL_THREADS) void balance_kernel(const float* __rest
   if (threadIdx.x == 0) *loss = gl_balance_loss(dot, total, E, k);
 }
 
-__global__ __launch_bounds__(GL_FINISH) void balance_finish_kernel(const float* __restrict__ part_p,
-                                                                   const int32_t* __restrict__ part_c, int blocks, int E,
-                                                                   int k, int32_t* __restrict__ counts,
-                                                                   float* __restrict__ prob_sum, float* __restrict__ loss) {
-  __shared__ double sp[GL_FINISH];
-  __shared__ int32_t sc[GL_FINISH];
-  __shared__ double sums[GL_FINISH / MOE_WAVE];
-  // `lanes` threads for a row of experts, the rows dealt to `groups` of them, eight rows on their way at a time
-  int lanes = 1;
-  while (lanes < E) lanes <<= 1;
-  const int groups = GL_FINISH / lanes, e = threadIdx.x % lanes, g = threadIdx.x / lanes;
-  double p = 0.0;
-  int32_t c = 0;
-  if (e < E)
-    for (int b = g; b < blocks; b += 8 * groups) {
-      float vp[8];
-      int32_t vc[8];
+// Adds the blocks' rows: L lanes of a wave (a power of two) for the experts of a row, four to a lane, so that a wave has
+// 64 / L rows at a time; the waves' sums meet in LDS.
+__global__ __launch_bounds__(GL_SUM_THREADS) void balance_finish_kernel(const float* __restrict__ part_p,
+                                                                        const int32_t* __restrict__ part_c, int blocks, int E,
+                                                                        int k, int L, int32_t* __restrict__ counts,
+                                                                        float* __restrict__ prob_sum, float* __restrict__ loss) {
+  constexpr int WAVES = GL_SUM_THREADS / MOE_WAVE;
+  __shared__ double sp[WAVES][MOE_MAX_E];
+  __shared__ int32_t sc[WAVES][MOE_MAX_E];
+  __shared__ double sums[WAVES];
+  const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, l = lane & (L - 1), pitch = gl_part_pitch(E);
+  const int rows = GL_SUM_THREADS / L;
+  double p[4] = {};
+  int32_t c[4] = {};
+  if (4 * l < E)
+    for (int b = threadIdx.x / L; b < blocks; b += 4 * rows) {
+      float4 vp[4];
+      int4 vc[4];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int64_t at = static_cast<int64_t>(b + u * groups) * E + e;
-        const bool there = b + u * groups < blocks;
-        vp[u] = there ? part_p[at] : 0.f;
-        vc[u] = there ? part_c[at] : 0;
+      for (int u = 0; u < 4; ++u) {
+        const int at = (b + u * rows) * pitch + 4 * l;
+        const bool there = b + u * rows < blocks;
+        vp[u] = there ? *reinterpret_cast<const float4*>(part_p + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+        vc[u] = there ? *reinterpret_cast<const int4*>(part_c + at) : make_int4(0, 0, 0, 0);
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        p += vp[u];
-        c += vc[u];
+      for (int u = 0; u < 4; ++u) {
+        p[0] += vp[u].x, p[1] += vp[u].y, p[2] += vp[u].z, p[3] += vp[u].w;
+        c[0] += vc[u].x, c[1] += vc[u].y, c[2] += vc[u].z, c[3] += vc[u].w;
       }
     }
-  sp[threadIdx.x] = p;
-  sc[threadIdx.x] = c;
+  for (int off = L; off < MOE_WAVE; off <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      p[j] += __shfl_xor(p[j], off);
+      c[j] += __shfl_xor(c[j], off);
+    }
+  if (lane < L && 4 * l < E)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sp[wave][4 * l + j] = p[j];
+      sc[wave][4 * l + j] = c[j];
+    }
   __syncthreads();
-  for (int half = groups / 2; half >= 1; half >>= 1) {
-    if (g < half) {
-      sp[threadIdx.x] += sp[threadIdx.x + half * lanes];
-      sc[threadIdx.x] += sc[threadIdx.x + half * lanes];
+  const int e = threadIdx.x;
+  double sum = 0.0;
+  int32_t count = 0;
+  if (e < E)
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      sum += sp[w][e];
+      count += sc[w][e];
     }
-    __syncthreads();
-  }
-  const bool mine = g == 0 && e < E;
-  p = mine ? sp[e] : 0.0;
-  c = mine ? sc[e] : 0;
-  const double total = gl_block_sum(static_cast<double>(c), sums);
-  const double dot = gl_block_sum(c * p, sums);
-  if (mine) {
-    counts[e] = c;
-    prob_sum[e] = static_cast<float>(p);
+  const double total = gl_block_sum(static_cast<double>(count), sums);
+  const double dot = gl_block_sum(count * sum, sums);
+  if (e < E) {
+    counts[e] = count;
+    prob_sum[e] = static_cast<float>(sum);
   }
   if (threadIdx.x == 0) *loss = gl_balance_loss(dot, total, E, k);
 }
@@ -284,58 +310,65 @@ __global__ __launch_bounds__(GL_FINISH) void balance_finish_kernel(const float* 
 //   renorm 0: w_j = p[i_j]:                 ds_e = p_e (g_e - sum_l p_l g_l),  g_e = sum of d_topk_w[j] with i_j = e
 //   renorm 1: w = softmax over the chosen:  ds[i_j] = w_j (d_topk_w[j] - sum_l w_l d_topk_w[l])
 //   balance:  b_e = coef E k c_e / (sum c)^2, ds_e = p_e (b_e - sum_l p_l b_l)
-template <int G, bool VEC>
+// ROUTING: d_topk_w is there.  ACC: d_scores is added to.
+template <int G, bool VEC, bool ROUTING, bool ACC>
 __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float* __restrict__ scores,
                                                                     const int32_t* __restrict__ topk_idx,
                                                                     const float* __restrict__ d_topk_w,
                                                                     const int32_t* __restrict__ counts, float coef,
                                                                     const uint8_t* __restrict__ mask, int T, int E, int k,
-                                                                    int renorm, int accumulate, int per_block,
-                                                                    float* __restrict__ d_scores) {
+                                                                    int renorm, int per_block, float* __restrict__ d_scores) {
   const int lane = lane_id(), l = lane % G;
   float b[4] = {};
-  if (counts) {
-    int64_t total = 0;
-    for (int e = lane; e < E; e += MOE_WAVE) total += counts[e];
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
-    const double c = total > 0 ? static_cast<double>(coef) * E * k / (static_cast<double>(total) * static_cast<double>(total)) : 0.0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int e = gl_expert<G, VEC>(l, j);
-      if (e < E) b[j] = static_cast<float>(c * counts[e]);
-    }
-  }
   const bool with_p = counts || !renorm;             // the softmax over all experts has a part in it
   struct Row {
-    float s[4], d[4];
+    float s[4], old[4], d[4];
     int e[4];
   };
   gl_rows<G, 2, Row>(
-      T, per_block, mask,
+      T, per_block, mask, scores,
       [&](Row& r, int64_t t) {
         gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
-        if (!d_topk_w) return;
-        // choices l, l + G, ... of the token are on lane l: k <= E <= 4 G
+        if constexpr (ACC) gl_load<G, VEC>(d_scores + t * E, E, l, 0.f, r.old);
+        if constexpr (ROUTING) {
+          // choices l, l + G, ... of the token are on lane l: k <= E <= 4 G
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int j = l + G * q;
-          r.e[q] = j < k ? topk_idx[t * k + j] : -1;
-          r.d[q] = j < k ? d_topk_w[t * k + j] : 0.f;
+          for (int q = 0; q < 4; ++q) {
+            const int64_t at = t * k + min(l + G * q, k - 1);
+            r.e[q] = topk_idx[at];
+            r.d[q] = d_topk_w[at];
+          }
         }
+      },
+      [&] {
+        if (!counts) return;
+        int64_t total = 0;
+        for (int e = lane; e < E; e += MOE_WAVE) total += counts[e];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int e = gl_expert<G, VEC>(l, j);
+          if (e < E) b[j] = static_cast<float>(counts[e]);
+        }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
+        const double n = static_cast<double>(total);
+        const float c = total > 0 ? static_cast<float>(static_cast<double>(coef) * E * k / (n * n)) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] *= c;
       },
       [&](Row& r, int64_t t, bool there, bool real) {
         float p[4] = {}, d[4] = {}, chosen[4] = {};
         if (with_p) gl_softmax<G>(r.s, p);
-        if (d_topk_w) {
+        if constexpr (ROUTING) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (static_cast<unsigned>(r.e[q]) >= static_cast<unsigned>(E)) r.e[q] = -1, r.d[q] = 0.f;
+            if (l + G * q >= k || static_cast<unsigned>(r.e[q]) >= static_cast<unsigned>(E)) r.e[q] = -1, r.d[q] = 0.f;
           if (renorm) {
             float w[4], m = -INFINITY, sum = 0.f, dot = 0.f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              w[q] = r.e[q] >= 0 ? scores[t * E + r.e[q]] : -INFINITY;
+              w[q] = scores[t * E + max(r.e[q], 0)];
+              w[q] = r.e[q] >= 0 ? w[q] : -INFINITY;
               m = fmaxf(m, w[q]);
             }
             m = gl_max<G>(m);
@@ -377,8 +410,11 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
           for (int j = 0; j < 4; ++j) d[j] = p[j] * (g[j] - dot);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) d[j] = real ? d[j] + (renorm ? chosen[j] : 0.f) : 0.f;
-        if (there && (real || !accumulate)) gl_store<G, VEC>(d_scores + t * E, E, l, accumulate, d);
+        for (int j = 0; j < 4; ++j) {
+          d[j] = real ? d[j] + (renorm ? chosen[j] : 0.f) : 0.f;
+          if constexpr (ACC) d[j] += r.old[j];
+        }
+        if (there && (real || !ACC)) gl_store<G, VEC>(d_scores + t * E, E, l, d);
       });
 }
 
@@ -400,7 +436,7 @@ __device__ __forceinline__ int gl_count_mask(const uint8_t* __restrict__ mask, i
 
 constexpr int GL_COUNT_BLOCKS = 64;
 __global__ __launch_bounds__(GL_THREADS) void mask_count_kernel(const uint8_t* __restrict__ mask, int T, int32_t* __restrict__ part) {
-  __shared__ int lds[GL_WAVES];
+  __shared__ int lds[GL_THREADS / MOE_WAVE];
   const int64_t per = (static_cast<int64_t>(T) + GL_COUNT_BLOCKS - 1) / GL_COUNT_BLOCKS;
   const int64_t begin = min(blockIdx.x * per, static_cast<int64_t>(T));
   const int n = gl_count_mask(mask, begin, min(begin + per, static_cast<int64_t>(T)), lds);
@@ -418,26 +454,31 @@ __device__ __forceinline__ double gl_tokens(const uint8_t* __restrict__ mask, co
 }
 static_assert(GL_COUNT_BLOCKS == MOE_WAVE, "one part per lane");
 
-template <int G, bool VEC>
+// ACC: d_scores is added to.
+template <int G, bool VEC, bool ACC>
 __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __restrict__ scores, const float* __restrict__ target,
                                                              const uint8_t* __restrict__ mask, const int32_t* __restrict__ part_n,
-                                                             int T, int E, float coef, int accumulate, int per_block,
+                                                             int T, int E, float coef, int per_block,
                                                              double* __restrict__ part_loss, float* __restrict__ loss,
                                                              float* __restrict__ d_scores) {
-  __shared__ double lds[GL_WAVES];
-  __shared__ int lds_n[GL_WAVES];
+  __shared__ double lds[GL_THREADS / MOE_WAVE];
+  __shared__ int lds_n[GL_THREADS / MOE_WAVE];
   const int lane = lane_id(), l = lane % G;
-  const double n = gl_tokens(mask, part_n, T, lds_n);
-  const float scale = n > 0.0 ? static_cast<float>(coef / n) : 0.f;
-  double sum = 0.0;
+  double n = 0.0, sum = 0.0;
+  float scale = 0.f;
   struct Row {
-    float s[4], u[4];
+    float s[4], u[4], old[4];
   };
   gl_rows<G, 2, Row>(
-      T, per_block, mask,
+      T, per_block, mask, scores,
       [&](Row& r, int64_t t) {
         gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
         gl_load<G, VEC>(target + t * E, E, l, -INFINITY, r.u);
+        if constexpr (ACC) gl_load<G, VEC>(d_scores + t * E, E, l, 0.f, r.old);
+      },
+      [&] {
+        n = gl_tokens(mask, part_n, T, lds_n);
+        scale = n > 0.0 ? static_cast<float>(coef / n) : 0.f;
       },
       [&](Row& r, int64_t t, bool there, bool real) {
         float p[4], q[4], lp[4], lq[4], d[4];
@@ -448,9 +489,10 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
         for (int j = 0; j < 4; ++j) {
           row += q[j] > 0.f ? q[j] * (lq[j] - lp[j]) : 0.f;      // q = 0 has no part
           d[j] = counts ? scale * (p[j] - q[j]) : 0.f;
+          if constexpr (ACC) d[j] += r.old[j];
         }
         sum += counts ? row : 0.f;
-        if (d_scores && there && (real || !accumulate)) gl_store<G, VEC>(d_scores + t * E, E, l, accumulate, d);
+        if (d_scores && there && (real || !ACC)) gl_store<G, VEC>(d_scores + t * E, E, l, d);
       });
   sum = gl_block_sum(sum * GL_LN2, lds);
   if (threadIdx.x != 0) return;
@@ -461,11 +503,11 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
 }
 
 // The mean of the blocks' losses.  (T == 0: no blocks, and 0.)
-__global__ __launch_bounds__(GL_FINISH) void distill_finish_kernel(const double* __restrict__ part_loss, int blocks,
+__global__ __launch_bounds__(GL_SUM_THREADS) void distill_finish_kernel(const double* __restrict__ part_loss, int blocks,
                                                                    const uint8_t* __restrict__ mask, const int32_t* __restrict__ part_n,
                                                                    int T, float* __restrict__ loss) {
-  __shared__ double lds[GL_FINISH / MOE_WAVE];
-  __shared__ int lds_n[GL_FINISH / MOE_WAVE];
+  __shared__ double lds[GL_SUM_THREADS / MOE_WAVE];
+  __shared__ int lds_n[GL_SUM_THREADS / MOE_WAVE];
   const double n = gl_tokens(mask, part_n, T, lds_n);
   const double sum = gl_block_sum(static_cast<int>(threadIdx.x) < blocks ? part_loss[threadIdx.x] : 0.0, lds);
   if (threadIdx.x == 0) *loss = n > 0.0 ? static_cast<float>(sum / n) : 0.f;
@@ -488,27 +530,37 @@ template <class F> static void gl_by_experts(int E, F f) {
   else with(std::integral_constant<int, 64>{});
 }
 
-// Blocks and rows of each.  A block that leaves partial sums takes 32 KiB of scores or more, and there are 256 of them at
-// most, as one block adds them up; what needs no sums takes 16 KiB and up to 2048 blocks.
+// Lanes that share a token.
+static int gl_lanes(int E) {
+  int g = 1;
+  while (4 * g < E) g <<= 1;
+  return g;
+}
+
+// Blocks of a call and the rows of each: a pass of the block's waves (U batches of rows each), or as many as the limit on
+// blocks asks for; a batch of up to `alone` passes is one block, which needs no launch to add up sums.
 struct GlPlan {
   int blocks, per_block;
 };
-static GlPlan gl_plan(int T, int E, bool sums) {
-  const int64_t least = (sums ? 8192 : 4096) / E + 1, most_blocks = sums ? 256 : 2048;
+static GlPlan gl_plan(int T, int E, int threads, int U, int alone, int most_blocks) {
+  const int64_t pass = static_cast<int64_t>(threads) / gl_lanes(E) * U;
   int64_t per = (static_cast<int64_t>(T) + most_blocks - 1) / most_blocks;
-  if (per < least) per = least;
-  const int rows = GL_WAVES * 64 / (E <= 4 ? 1 : E <= 8 ? 2 : E <= 16 ? 4 : E <= 32 ? 8 : E <= 64 ? 16 : E <= 128 ? 32 : 64);
-  per = (per + rows - 1) / rows * rows;
-  if (per > T) per = T;
+  per = (per + pass - 1) / pass * pass;
+  if (T <= alone * pass) per = T;
   return {T > 0 ? static_cast<int>((T + per - 1) / per) : 0, static_cast<int>(per)};
 }
+// Sums for every expert: one block adds up the blocks' rows, so there are 256 blocks at most.
+static GlPlan gl_balance_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_SUM_THREADS, 2, 2, 256); }
+// One sum: as many blocks as the finishing block has threads.
+static GlPlan gl_distill_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 2, 4, GL_SUM_THREADS); }
+static GlPlan gl_route_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 2, 1, 1024); }
 
 // From this many tokens on the mask is counted by a launch of its own, not by every block.
 constexpr int GL_COUNT_FROM = 1 << 14;
 
 size_t gate_loss_workspace_bytes(const moe_shape_t* shape) {
-  const size_t b = static_cast<size_t>(gl_plan(shape->T, shape->E, true).blocks);
-  const size_t balance = b > 1 ? b * shape->E * 8 : 0, distill = b * 8 + GL_COUNT_BLOCKS * 4;
+  const size_t balance = static_cast<size_t>(gl_balance_plan(shape).blocks) * gl_part_pitch(shape->E) * 8;
+  const size_t distill = static_cast<size_t>(gl_distill_plan(shape).blocks) * 8 + GL_COUNT_BLOCKS * 4;
   return balance > distill ? balance : distill;
 }
 
@@ -526,16 +578,17 @@ extern "C" int moe_balance_loss(const moe_shape_t* shape, const float* scores, c
   if (workspace_bytes < gate_loss_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E, k = shape->k;
-  const GlPlan plan = gl_plan(T, E, true);
+  const GlPlan plan = gl_balance_plan(shape);
   float* part_p = static_cast<float*>(workspace);
-  int32_t* part_c = reinterpret_cast<int32_t*>(part_p + static_cast<size_t>(plan.blocks) * E);
+  int32_t* part_c = reinterpret_cast<int32_t*>(part_p + static_cast<size_t>(plan.blocks) * gl_part_pitch(E));
   if (T > 0)
     gl_by_experts(E, [&](auto g, auto vec) {
-      hipLaunchKernelGGL((balance_kernel<g(), vec()>), dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, topk_idx, token_mask, T, E, k,
+      hipLaunchKernelGGL((balance_kernel<decltype(g)::value, decltype(vec)::value>), dim3(plan.blocks), dim3(GL_SUM_THREADS), 0, st, scores, topk_idx, token_mask, T, E, k,
                          plan.per_block, part_p, part_c, counts, prob_sum, loss);
     });
   if (plan.blocks != 1)
-    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(GL_FINISH), 0, st, part_p, part_c, plan.blocks, E, k, counts, prob_sum, loss);
+    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(GL_SUM_THREADS), 0, st, part_p, part_c, plan.blocks, E, k, gl_lanes(E), counts,
+                       prob_sum, loss);
   return launch_status();
 }
 
@@ -553,10 +606,14 @@ extern "C" int moe_route_backward(const moe_shape_t* shape, const float* scores,
     return MOE_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E, k = shape->k;
-  const GlPlan plan = gl_plan(T, E, false);
+  const GlPlan plan = gl_route_plan(shape);
   gl_by_experts(E, [&](auto g, auto vec) {
-    hipLaunchKernelGGL((route_backward_kernel<g(), vec()>), dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, topk_idx, d_topk_w, counts,
-                       balance_coef, token_mask, T, E, k, shape->renorm, accumulate, plan.per_block, d_scores);
+    constexpr int G = decltype(g)::value;
+    constexpr bool VEC = decltype(vec)::value;
+    const auto kernel = d_topk_w ? (accumulate ? route_backward_kernel<G, VEC, true, true> : route_backward_kernel<G, VEC, true, false>)
+                                 : (accumulate ? route_backward_kernel<G, VEC, false, true> : route_backward_kernel<G, VEC, false, false>);
+    hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, topk_idx, d_topk_w, counts, balance_coef, token_mask, T, E,
+                       k, shape->renorm, plan.per_block, d_scores);
   });
   return launch_status();
 }
@@ -574,7 +631,7 @@ extern "C" int moe_gate_distill(const moe_shape_t* shape, const float* scores, c
   if (workspace_bytes < gate_loss_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E;
-  const GlPlan plan = gl_plan(T, E, true);
+  const GlPlan plan = gl_distill_plan(shape);
   double* part_loss = static_cast<double*>(workspace);
   int32_t* part_n = nullptr;
   if (token_mask && T >= GL_COUNT_FROM) {
@@ -583,10 +640,13 @@ extern "C" int moe_gate_distill(const moe_shape_t* shape, const float* scores, c
   }
   if (T > 0)
     gl_by_experts(E, [&](auto g, auto vec) {
-      hipLaunchKernelGGL((distill_kernel<g(), vec()>), dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, target_scores, token_mask, part_n, T,
-                         E, coef, accumulate, plan.per_block, part_loss, loss, d_scores);
+      constexpr int G = decltype(g)::value;
+      constexpr bool VEC = decltype(vec)::value;
+      const auto kernel = accumulate && d_scores ? distill_kernel<G, VEC, true> : distill_kernel<G, VEC, false>;
+      hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, target_scores, token_mask, part_n, T, E, coef,
+                         plan.per_block, part_loss, loss, d_scores);
     });
   if (plan.blocks != 1)
-    hipLaunchKernelGGL(distill_finish_kernel, dim3(1), dim3(GL_FINISH), 0, st, part_loss, plan.blocks, token_mask, part_n, T, loss);
+    hipLaunchKernelGGL(distill_finish_kernel, dim3(1), dim3(GL_SUM_THREADS), 0, st, part_loss, plan.blocks, token_mask, part_n, T, loss);
   return launch_status();
 }
