@@ -60,7 +60,9 @@ template <bool BF16, int V> struct GbFrag {
 // behind a branch, so that the waits for one step's operands can leave the next one's on their way.
 constexpr uint32_t GB_NOWHERE = 0x80000000u;          // a place outside every descriptor (with a few rows added as well)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t gb_rows(const void* first, int rows, uint32_t pitch) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, static_cast<int>(static_cast<uint32_t>(max(rows, 0)) * pitch), 0x00020000);
+  // (the clamp may become an instruction of the vector unit; a descriptor has to be in scalar registers)
+  const uint32_t n = __builtin_amdgcn_readfirstlane(max(rows, 0));
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, static_cast<int>(n * pitch), 0x00020000);
 }
 __device__ __forceinline__ float gb_load_f32(__amdgpu_buffer_rsrc_t rows, uint32_t at) {
   return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rows, static_cast<int>(at), 0, 0));
@@ -155,17 +157,9 @@ __device__ __forceinline__ GwPlace gw_place(int tiles, int chunks, int splits) {
   return {rest / chunks, rest % chunks, splits % 8 == 0 ? b / 8 / n * 8 + b % 8 : b / n};
 }
 
-// What a wave multiplies in one step: 32 tokens, lane 16 g + c the tokens 8 g + 0..7 of its columns and experts.
-template <bool BF16, int MT, int V> struct GwStep {
-  GbRow<BF16, V> x[8];
-  float ds[MT][8];
-  uint32_t mask;         // of token t0 + (lane & 31)
-  int left;              // tokens from t0 to the end
-};
-
 // Up to 32 experts: a lane loads the values of d_scores that it needs (8 tokens of an expert) one by one.
 template <bool BF16, int MT, int V>
-__global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(GwArgs a) {
+__global__ __launch_bounds__(GW_THREADS, MT == 1 ? 4 : 2) void gate_weight_kernel(GwArgs a) {
   constexpr int B = BF16 ? 2 : 4;
   __shared__ gb_f32x4 red[GW_WAVES][4][MOE_WAVE];
   __shared__ float red_b[GW_WAVES][16 * MT];
@@ -190,62 +184,58 @@ __global__ __launch_bounds__(GW_THREADS) void gate_weight_kernel(GwArgs a) {
     for (int i = 0; i < V; ++i) acc[m][i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  using Step = GwStep<BF16, MT, V>;
-  auto load = [&](Step& s, uint32_t t0) {
-    s.left = static_cast<int>(end - t0);
+  // What a wave multiplies in one step: 32 tokens, lane 16 g + c the tokens 8 g + 0..7 of its columns and experts.
+  GbRow<BF16, V> x[8];
+  float ds[MT][8];
+  uint32_t mask;                                     // of token t0 + (lane & 31)
+  auto load = [&](uint32_t t0) {
+    const int left = min(static_cast<int>(end - t0), 32);
     // a descriptor for every row that the lanes have in common: what differs between lanes stays the same
     const char* x0 = a.x + static_cast<int64_t>(t0) * pitch;
     const char* s0 = reinterpret_cast<const char*>(a.d_scores) + static_cast<int64_t>(t0) * pitch_s;
-    s.mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? min(s.left, 32) : 0, 1), lane & 31, 0, 0);
+    mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t0, a.mask ? left : 0, 1), lane & 31, 0, 0);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        s.ds[m][j] = gb_load_f32(gb_rows(s0 + j * pitch_s, min(s.left, 32) - j, pitch_s),
-                                 8 * g * pitch_s + static_cast<uint32_t>(min(16 * m + c, E - 1)) * 4);
+        ds[m][j] = gb_load_f32(gb_rows(s0 + j * pitch_s, left - j, pitch_s),
+                               8 * g * pitch_s + static_cast<uint32_t>(min(16 * m + c, E - 1)) * 4);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s.x[j].load(gb_rows(x0 + static_cast<int64_t>(j) * pitch, with_w ? min(s.left, 32) - j : 0, pitch), at_x);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int j = 0; j < 8; ++j) x[j].load(gb_rows(x0 + static_cast<int64_t>(j) * pitch, with_w ? left - j : 0, pitch), at_x);
   };
-  auto multiply = [&](Step& s) {
-    if (a.mask || s.left < 32) {
+  // A step's operands go over to the registers that the products read, and the next step's are requested into the ones
+  // that are free then; behind the last step nothing is read.
+  uint32_t t0 = begin + 32 * wave;
+  load(t0);
+  while (t0 < end) {
+    const int left = static_cast<int>(end - t0);
+    if (a.mask || left < 32) {
       // bit j: token t0 + 8 g + j counts
-      const uint32_t real = static_cast<uint32_t>(__ballot((lane & 31) < s.left && (!a.mask || s.mask))) >> (8 * g);
+      const uint32_t real = static_cast<uint32_t>(__ballot((lane & 31) < left && (!a.mask || mask))) >> (8 * g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        s.x[j].keep(real >> j & 1);
+        x[j].keep(real >> j & 1);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) s.ds[m][j] = real >> j & 1 ? s.ds[m][j] : 0.f;
+        for (int m = 0; m < MT; ++m) ds[m][j] = real >> j & 1 ? ds[m][j] : 0.f;
       }
     }
     GbFrag<BF16, V> b;
-    gb_transpose<BF16, V>(s.x, b);
+    gb_transpose<BF16, V>(x, b);
+    uint4 p[MT][3];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       if (with_bias) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bias[m] += s.ds[m][j];
+        for (int j = 0; j < 8; ++j) bias[m] += ds[m][j];
       }
-      uint4 p[3];
-      gb_split8(s.ds[m], p);
-      gb_products<BF16, false, V>(p[0], p[1], p[2], b, acc[m]);
+      gb_split8(ds[m], p[m]);
     }
     __builtin_amdgcn_sched_barrier(0);
-  };
-  // the next step's operands are on their way while this one's are multiplied; behind the last step nothing is read
-  {
-    Step s0, s1;
-    uint32_t t0 = begin + 32 * wave;
-    load(s0, t0);
-    while (t0 < end) {
-      load(s1, t0 + 32 * GW_WAVES);
-      multiply(s0);
-      t0 += 32 * GW_WAVES;
-      if (t0 >= end) break;
-      load(s0, t0 + 32 * GW_WAVES);
-      multiply(s1);
-      t0 += 32 * GW_WAVES;
-    }
+    t0 += 32 * GW_WAVES;
+    load(t0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) gb_products<BF16, false, V>(p[m][0], p[m][1], p[m][2], b, acc[m]);
   }
 
   // sums of the waves, 16 experts at a time: lane 16 g + c of a wave holds experts 4 g + 0..3 of the columns V c + i
