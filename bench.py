@@ -161,6 +161,44 @@ def calibration_copy(torch):
     torch.cuda.synchronize()
 
 
+def predictor_finetune(torch, si, B, layer, cfg, L, steps):
+    """Fine-tunes a load predictor on a synthetic residual stream (outside the timed region): the hidden states one
+    layer later are x (1 + 0.5 g) + 0.1 n with a fixed gain g per channel, so that the later layer's gate, applied to x,
+    is a start that leaves something to learn.  Trained on 70 % of the batch's tokens, measured on the other 30 %."""
+    n = cfg.T * 7 // 10
+    gen = torch.Generator(device="cuda").manual_seed(cfg.seed)
+    x = layer.to_device(L["x"])
+    gain = torch.randn((cfg.d,), device="cuda", generator=gen)
+    noise = torch.randn((cfg.T, cfg.d), device="cuda", generator=gen)
+    later = (x.float() * (1 + 0.5 * gain) + 0.1 * noise).to(x.dtype)
+    w_later = layer.to_device(si.make_layer(
+        si.small_config("predictor_gate", T=cfg.T, d=cfg.d, E=cfg.E, k=cfg.k, F=cfg.F, dtype=cfg.dtype,
+                        renorm=cfg.renorm, seed=cfg.seed + 1), parts=("w_gate",))["w_gate"])
+    trainer = layer.GateTrainer(n, cfg.d, cfg.E, cfg.k, 1, cfg.dtype, cfg.renorm)
+    target = torch.empty((n, cfg.E), dtype=torch.float32, device="cuda")
+    trainer.score(later[:n], w_later, target)
+    test = layer.LoadPredictor(cfg.T - n, cfg.d, cfg.E, cfg.k, cfg.dtype, cfg.renorm, cfg.E)
+
+    def kept(w):
+        return layer.predicted_vs_actual_loads(test, x[n:], later[n:], w, w_later=w_later)[2]
+
+    before = kept(w_later)
+    w, losses = layer.finetune_predictor(trainer, x[:n], target, w_later, steps, 0.1 / cfg.d ** 0.5)
+    us = {}
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    for name, f in (("losses_and_gradients", lambda: trainer.enqueue(0, x[:n], w, target)), ("clip", trainer.clip)):
+        f()
+        start.record()
+        for _ in range(20):
+            f()
+        end.record()
+        end.synchronize()
+        us[name + "_us"] = start.elapsed_time(end) / 20 * 1e3
+    return {"model": "x_later = x (1 + 0.5 g) + 0.1 N(0,1), g per channel; start: the later layer's gate",
+            "tokens": n, "held_out_tokens": cfg.T - n, "steps": steps, "loss_first": losses[0], "loss_last": losses[-1],
+            "token_choices_kept_before": before, "token_choices_kept_after": kept(w), **us}
+
+
 def hbm_bound_calls(torch, si, B, layer, st):
     """moe_route, moe_count_and_permute (with the row copy) and moe_combine at a bandwidth-bound
     batch: average time of HBM_BOUND_ITERS launches each (HIP events on the launch stream), two
@@ -241,6 +279,9 @@ def main():
     ap.add_argument("--predictor-accuracy", action="store_true",
                     help="also report how the loads predicted from x match those the same gate gives "
                          "on x + eps * noise (a residual-stream stand-in), for several eps")
+    ap.add_argument("--predictor-finetune", type=int, default=0, metavar="K",
+                    help="also fine-tune a load predictor for K steps on a synthetic residual stream and "
+                         "report the token choices it gets right before and after, on held-out tokens")
     ap.add_argument("--tokens", type=int, default=0, metavar="T",
                     help="run the workload's layer on a batch of T tokens instead of its own size "
                          "(same seeds and shapes otherwise; the JSON line names the batch)")
@@ -524,6 +565,8 @@ def main():
                      "layer's gate (a second seeded gate matrix) applied to x, the truth the same gate "
                      "on x_later; the workload's gate bias is applied to both",
             "rows": rows}
+    if args.predictor_finetune > 0:
+        out["predictor_finetune"] = predictor_finetune(torch, si, B, layer, cfg, L, args.predictor_finetune)
     if args.ep_sim > 0:
         # outside the timed region: the permuted rows are materialised once, then every simulated
         # rank's grouped FFN runs alone

@@ -151,10 +151,95 @@ class LoadPredictor:
             self.round += 1
 
 
-def predicted_vs_actual_loads(pred: LoadPredictor, x_now, x_later, w_pred, gate_bias=None, stream=None):
-    """How well the loads predicted from the current hidden states match those the same gate sees
-    one layer later (paper, Section 4.1 and its accuracy study): both passes are the library's
-    routing and counting; the comparison of the two small count vectors is host arithmetic.
+class GateTrainer:
+    """Gradients of gates, for fine-tuning load predictors (paper, Section 4.1: a predictor is a copy of a later layer's
+    gate, trained on stored hidden states and that gate's outputs) or for the load balance of routers.  One step:
+
+        for i in range(n_gates):
+            trainer.enqueue(i, x[i], w_gate[i], target_scores[i])     # loss and gradients of gate i
+        trainer.clip()                                               # over the gradients of all gates
+        ...                                                           # the caller's optimizer, on d_w_gate and d_gate_bias
+
+    enqueue() = moe_route_ws (scores of the gate) -> moe_gate_distill -> moe_balance_loss -> moe_route_backward (with a
+    balance_coef) -> moe_gate_backward.  Everything is enqueued on one stream; nothing is read back to the host, and
+    nothing is allocated.  Outputs: `loss`, `balance` [n_gates] (the distillation and the balance loss), `counts`
+    [n_gates, E], `d_w_gate` [n_gates, E, d] and `d_gate_bias` [n_gates, E] in fp32, and `norm` [1] of clip().  All gates
+    share the trainer's workspace: use one stream at a time."""
+
+    def __init__(self, T, d, E, k, n_gates, dtype, renorm, max_norm=1.0, balance_coef=0.0, device="cuda"):
+        # F does not enter any of the calls used here; 8 keeps the shape valid for both dtypes
+        self.shape = B.make_shape(T, d, E, k, 8, dtype, renorm)
+        self.n_gates = int(n_gates)
+        self.max_norm, self.balance_coef = float(max_norm), float(balance_coef)
+        kw = dict(device=device)
+        self.topk_idx = torch.empty((T, k), dtype=torch.int32, **kw)
+        self.topk_w = torch.empty((T, k), dtype=torch.float32, **kw)
+        self.scores = torch.empty((T, E), dtype=torch.float32, **kw)
+        self.d_scores = torch.empty((T, E), dtype=torch.float32, **kw)
+        self.prob_sum = torch.empty((E,), dtype=torch.float32, **kw)
+        self.counts = torch.zeros((n_gates, E), dtype=torch.int32, **kw)
+        self.loss = torch.zeros((n_gates,), dtype=torch.float32, **kw)
+        self.balance = torch.zeros((n_gates,), dtype=torch.float32, **kw)
+        self.d_w_gate = torch.zeros((n_gates, E, d), dtype=torch.float32, **kw)
+        self.d_gate_bias = torch.zeros((n_gates, E), dtype=torch.float32, **kw)
+        self.grads = B.GradList([t for i in range(n_gates) for t in (self.d_w_gate[i], self.d_gate_bias[i])])
+        self.norm = torch.zeros((1,), dtype=torch.float32, **kw)
+        # one buffer: the calls of a step follow each other on a stream
+        self.ws_bytes = max(B.moe_workspace_bytes(self.shape), B.moe_train_workspace_bytes(self.shape),
+                            B.moe_grad_workspace_bytes(self.grads))
+        self.workspace = torch.empty((self.ws_bytes,), dtype=torch.uint8, **kw)
+
+    def score(self, x, w_gate, scores, gate_bias=None, stream=None):
+        """The scores [T, E] of a gate on x: targets for the gates that predict it."""
+        s = torch.cuda.current_stream() if stream is None else stream
+        B.moe_route_ws(self.shape, x, w_gate, gate_bias, self.topk_idx, self.topk_w, scores, self.workspace,
+                       self.ws_bytes, s)
+
+    def enqueue(self, i, x, w_gate, target_scores, gate_bias=None, token_mask=None, accumulate=False, d_x=None,
+                stream=None):
+        """Losses and gradients of gate i.  token_mask: 0 for padded tokens.  accumulate: the gradients are added to
+        those of earlier micro-batches (before clip()).  d_x: an output for the hidden states' gradient, or None."""
+        s = torch.cuda.current_stream() if stream is None else stream
+        ws, nb = self.workspace, self.ws_bytes
+        self.score(x, w_gate, self.scores, gate_bias, s)
+        B.moe_gate_distill(self.shape, self.scores, target_scores, token_mask, 1.0, self.loss[i:i + 1], self.d_scores, 0,
+                           ws, nb, s)
+        B.moe_balance_loss(self.shape, self.scores, self.topk_idx, token_mask, self.counts[i], self.prob_sum,
+                           self.balance[i:i + 1], ws, nb, s)
+        if self.balance_coef != 0.0:
+            B.moe_route_backward(self.shape, self.scores, None, None, self.counts[i], self.balance_coef, token_mask,
+                                 self.d_scores, 1, s)
+        B.moe_gate_backward(self.shape, x, None if d_x is None else w_gate, self.d_scores, token_mask, self.d_w_gate[i],
+                            self.d_gate_bias[i], d_x, B.MOE_ACCUMULATE_WEIGHTS if accumulate else 0, ws, nb, s)
+
+    def clip(self, stream=None):
+        """Scales the gradients of all gates, in place, to a norm of at most max_norm; returns `norm` (on the device)."""
+        s = torch.cuda.current_stream() if stream is None else stream
+        B.moe_clip_grads(self.grads, self.max_norm, self.norm, self.workspace, self.ws_bytes, s)
+        return self.norm
+
+
+def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps, lr, token_mask=None):
+    """Fine-tunes gate 0 of `trainer`, starting from w_gate: predictor of `target_scores` from x_now.  Returns the new
+    weights in w_gate's type and the losses of the steps.  The optimizer is PyTorch's Adam on an fp32 copy."""
+    master = w_gate.float().clone().requires_grad_(True)
+    opt = torch.optim.Adam([master], lr=lr)
+    w, losses = w_gate.clone(), []
+    for _ in range(steps):
+        trainer.enqueue(0, x_now, w, target_scores, token_mask=token_mask)
+        trainer.clip()
+        losses.append(trainer.loss[0].clone())
+        master.grad = trainer.d_w_gate[0]
+        opt.step()
+        with torch.no_grad():
+            w.copy_(master)
+    return w, [float(v) for v in losses]
+
+
+def predicted_vs_actual_loads(pred: LoadPredictor, x_now, x_later, w_pred, gate_bias=None, stream=None, w_later=None):
+    """How well the loads predicted from the current hidden states match those the same gate (or w_later, the gate
+    that w_pred was fine-tuned to predict) sees one layer later (paper, Section 4.1 and its accuracy study): both
+    passes are the library's routing and counting; the comparison of the two small count vectors is host arithmetic.
     Returns (predicted counts, actual counts, fraction of (token, slot) choices that the later
     routing also makes for that token)."""
     s = torch.cuda.current_stream() if stream is None else stream
@@ -162,7 +247,7 @@ def predicted_vs_actual_loads(pred: LoadPredictor, x_now, x_later, w_pred, gate_
     with torch.cuda.stream(s):
         c_pred = pred.counts.clone()
         idx_pred = pred.topk_idx.clone()
-    pred.enqueue(x_later, w_pred, gate_bias, stream=s)
+    pred.enqueue(x_later, w_pred if w_later is None else w_later, gate_bias, stream=s)
     with torch.cuda.stream(s):
         same = (idx_pred.unsqueeze(2) == pred.topk_idx.unsqueeze(1)).any(dim=2).float().mean()
     s.synchronize()

@@ -574,6 +574,58 @@ def test_two_steps_at_once_on_two_streams():
         assert all(torch.equal(ref[n], got[n]) for n in ref)
 
 
+@pytest.mark.parametrize("dtype,balance_coef", [(B.MOE_BF16, 0.0), (B.MOE_BF16, 0.05), (B.MOE_F32, 0.05)])
+def test_gate_trainer_against_the_oracle(dtype, balance_coef):
+    """Two gates, one of them in two micro-batches, a padded batch, d_x, and the clipped gradients of both."""
+    T, d, E, k, n = 130, 72, 20, 3, 2
+    rng = np.random.default_rng(31)
+    tr = layer.GateTrainer(T, d, E, k, n, dtype, 1, max_norm=0.05, balance_coef=balance_coef)
+    mask = mask_of("some", T, 31)
+    sums, norms = [], 0.0
+    for i in range(n):
+        dw_sum, db_sum = np.zeros((E, d)), np.zeros(E)
+        for micro in range(1 + i):
+            x, w = store(rng.standard_normal((T, d)), dtype), store(rng.standard_normal((E, d)) / np.sqrt(d), dtype)
+            target = rng.standard_normal((T, E)).astype(np.float32)
+            d_x = torch.zeros((T, d), dtype=torch.float32 if dtype == B.MOE_F32 else torch.bfloat16, device="cuda")
+            tr.enqueue(i, layer.to_device(x), layer.to_device(w), dev(target), token_mask=dev(mask), accumulate=micro > 0, d_x=d_x)
+            scores, idx = tr.scores.cpu().numpy(), tr.topk_idx.cpu().numpy()
+            assert np.abs(scores - orc.gate_scores(x, w)).max() <= 1e-4
+            loss, g = go.gate_distill(scores, target, 1.0, mask)
+            counts, _, balance = go.balance_loss(scores, idx, mask)
+            if balance_coef:
+                g = g + go.route_backward(scores, idx, None, counts, balance_coef, 1, mask, k)
+            dw, db, dx = go.gate_backward(orc.to_f64(x), orc.to_f64(w), g, mask)
+            dw_sum, db_sum = dw_sum + dw, db_sum + db
+            assert float(tr.loss[i]) == pytest.approx(loss, rel=1e-5) and float(tr.balance[i]) == pytest.approx(balance, rel=1e-5)
+            assert np.array_equal(tr.counts[i].cpu().numpy(), counts)
+            half = 2.0 ** -8 if dtype == B.MOE_BF16 else 1e-5
+            assert np.abs(d_x.double().cpu().numpy() - dx).max() <= half * np.abs(dx).max() + 1e-5 * np.abs(dx).max()
+        assert np.abs(tr.d_w_gate[i].cpu().numpy() - dw_sum).max() <= 1e-5 * np.abs(dw_sum).max()
+        assert np.abs(tr.d_gate_bias[i].cpu().numpy() - db_sum).max() <= 1e-5 * np.abs(dw_sum).max()
+        sums.append((dw_sum, db_sum))
+    norm, clipped = go.clip_grads([t for pair in sums for t in pair], 0.05)
+    assert float(tr.clip()) == pytest.approx(norm, rel=1e-5)
+    for i in range(n):
+        assert np.abs(tr.d_w_gate[i].cpu().numpy() - clipped[2 * i]).max() <= 1e-5 * np.abs(clipped[2 * i]).max()
+
+
+def test_finetuning_runs():
+    T, d, E, k = 300, 64, 8, 2
+    cfg = si.small_config(T=T, d=d, E=E, k=k, F=64, seed=33)
+    L = si.make_layer(cfg, parts=("x", "w_gate"))
+    x, w = layer.to_device(L["x"]), layer.to_device(L["w_gate"])
+    tr = layer.GateTrainer(T, d, E, k, 1, cfg.dtype, cfg.renorm)
+    target = torch.empty((T, E), device="cuda")
+    tr.score(torch.roll(x, 1, 1).contiguous(), w, target)
+    new, losses = layer.finetune_predictor(tr, x, target, w, 3, 1e-3)
+    assert new.shape == w.shape and new.dtype == w.dtype and len(losses) == 3 and np.isfinite(losses).all()
+    test = layer.LoadPredictor(T, d, E, k, cfg.dtype, cfg.renorm, E)
+    pred, true, kept = layer.predicted_vs_actual_loads(test, x, x, new, w_later=w)
+    assert pred.sum() == true.sum() == T * k and 0.0 <= kept <= 1.0
+    assert layer.predicted_vs_actual_loads(test, x, x, w)[2] == 1.0
+
+
 def test_an_empty_batch_gives_zeros_or_leaves_what_is_there():
     for E in (1, 8, 200):
         sh = shape_of(0, E, 1, 0, 64)
