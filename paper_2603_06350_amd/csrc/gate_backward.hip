@@ -151,21 +151,21 @@ struct GwArgs {
 struct GwPlace {
   int tile, chunk, split;
 };
-__device__ __forceinline__ GwPlace gw_place(int tiles, int chunks, int splits) {
-  const int n = tiles * chunks, b = blockIdx.x;
+__device__ __forceinline__ GwPlace gw_place(int tiles, int chunks, int splits, int b) {
+  const int n = tiles * chunks;
   const int rest = splits % 8 == 0 ? b / 8 % n : b % n;
   return {rest / chunks, rest % chunks, splits % 8 == 0 ? b / 8 / n * 8 + b % 8 : b / n};
 }
 
 // Up to 32 experts: a lane loads the values of d_scores that it needs (8 tokens of an expert) one by one.
+constexpr int GW_LDS = GW_WAVES * 4 * MOE_WAVE * 16;
 template <bool BF16, int MT, int V>
-__global__ __launch_bounds__(GW_THREADS, MT == 1 ? 4 : 2) void gate_weight_kernel(GwArgs a) {
+__device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, unsigned char* lds, float (*red_b)[16 * MT]) {
   constexpr int B = BF16 ? 2 : 4;
-  __shared__ gb_f32x4 red[GW_WAVES][4][MOE_WAVE];
-  __shared__ float red_b[GW_WAVES][16 * MT];
+  auto red = reinterpret_cast<gb_f32x4(*)[4][MOE_WAVE]>(lds);
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
   const int d = a.d, E = a.E, splits = a.splits;
-  const GwPlace at_block = gw_place(a.tiles, 1, splits);
+  const GwPlace at_block = gw_place(a.tiles, 1, splits, block);
   const int tile = at_block.tile, split = at_block.split;
   // (token numbers in 32 unsigned bits: T < 2^31, and no number passes it by more than the blocks' steps)
   const uint32_t begin = static_cast<uint32_t>(split) * a.per_split;
@@ -300,7 +300,7 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
   const int half = wave >> 2;
   const int d = a.d, E = a.E, splits = a.splits;
-  const GwPlace place = gw_place(a.tiles, (E + 63) / 64, splits);
+  const GwPlace place = gw_place(a.tiles, (E + 63) / 64, splits, blockIdx.x);
   const int e0 = place.chunk * 64;
   const uint32_t begin = static_cast<uint32_t>(place.split) * a.per_split;
   const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
@@ -493,8 +493,7 @@ __global__ __launch_bounds__(GS_THREADS) void gate_sum_kernel(const float* __res
 // block lie side by side and run over tokens, GT at a time.  The block reads d_scores of its next GT tokens in whole
 // rows, cuts them into pieces once and keeps these in LDS, from where the waves take their operands.  (Every wave
 // reading its operands straight from global memory: 64 lanes in 64 places, which the L1 serves one after the other; XXX.)
-constexpr int GX_THREADS = 256;
-constexpr int GX_WAVES = GX_THREADS / MOE_WAVE;
+constexpr int GX_SIDE = 4;                            // waves side by side
 
 struct GxArgs {
   const char* w_gate;
@@ -504,47 +503,43 @@ struct GxArgs {
   int T, d, E, tiles, splits, per_split;
 };
 
-template <bool BF16, int KS> struct GxTile {
+// THREADS: 256, or 512 for two groups of waves side by side, each with GT tokens of a step of its own.
+template <bool BF16, int KS, int THREADS> struct GxTile {
   static constexpr int P = BF16 ? 2 : 3;             // pieces of d_scores
-  static constexpr int GT = KS <= 2 ? 64 : 128 / KS; // tokens of a step
+  static constexpr int GT = KS <= 2 ? 64 : 128 / KS; // tokens of a wave's step
+  static constexpr int STEP = GT * THREADS / 256;    // tokens of the block's step
   static constexpr int CPT = 8 * KS;                 // chunks of four experts of a token
-  static constexpr int LOADS = GT * CPT / GX_THREADS;
+  static constexpr int LOADS = STEP * CPT / THREADS;
   static constexpr int PITCH = 64 * KS + 16;         // bytes of a row in LDS: 16 more than the experts take, against bank conflicts
+  static constexpr int PIECE = STEP * PITCH;
+  static constexpr int LDS = 2 * P * PIECE;
 };
 
 // WHOLE: E is a multiple of 4, so that rows of d_scores are whole 16-byte chunks.  ACC: d_x is added to.
-template <bool BF16, int KS, int V, bool WHOLE, bool ACC>
-__global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxArgs a) {
-  using Tile = GxTile<BF16, KS>;
-  constexpr int B = BF16 ? 2 : 4, P = Tile::P, GT = Tile::GT, CPT = Tile::CPT, LOADS = Tile::LOADS, PITCH = Tile::PITCH;
-  __shared__ __align__(16) unsigned char pieces[2][P][GT * PITCH];
-  __shared__ uint32_t reals[2][GT / 4];              // a byte per token: it counts (ACC)
+template <bool BF16, int KS, int V, int THREADS, bool WHOLE, bool ACC>
+__device__ __forceinline__ void gate_x_block(const GxArgs& a, int block, unsigned char* lds, uint32_t* reals) {
+  using Tile = GxTile<BF16, KS, THREADS>;
+  constexpr int B = BF16 ? 2 : 4, P = Tile::P, GT = Tile::GT, STEP = Tile::STEP, CPT = Tile::CPT, LOADS = Tile::LOADS, PITCH = Tile::PITCH,
+                PIECE = Tile::PIECE;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
-  const int d = a.d, E = a.E;
-  int split, tile;                                   // as in gate_weight_kernel
-  if (a.splits % 8 == 0) {
-    tile = blockIdx.x / 8 % a.tiles;
-    split = blockIdx.x / 8 / a.tiles * 8 + blockIdx.x % 8;
-  } else {
-    tile = blockIdx.x % a.tiles;
-    split = blockIdx.x / a.tiles;
-  }
-  const int col = (tile * GX_WAVES + wave) * 16 * V + V * c;
-  const uint32_t begin = static_cast<uint32_t>(split) * a.per_split;
+  const int d = a.d, E = a.E, first = wave / GX_SIDE * GT;             // of this wave's tokens in a step
+  const GwPlace place = gw_place(a.tiles, 1, a.splits, block);
+  const int col = (place.tile * GX_SIDE + wave % GX_SIDE) * 16 * V + V * c;
+  const uint32_t begin = static_cast<uint32_t>(place.split) * a.per_split;
   const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
   if (begin >= end) return;                          // the whole block
   const uint32_t pitch = static_cast<uint32_t>(d) * B, pitch_s = static_cast<uint32_t>(E) * 4;
 
-  // Chunk threadIdx.x + 256 i of a step: four experts of one token.
+  // Chunk threadIdx.x + THREADS i of a step: four experts of one token.
   float v[LOADS][4];
   uint32_t mask[LOADS];
   auto load = [&](uint32_t t0) {
-    const int rows = min(static_cast<int>(end - t0), GT);
+    const int rows = min(static_cast<int>(end - t0), STEP);
     const auto sr = gb_rows(a.d_scores + static_cast<int64_t>(t0) * E, rows, pitch_s);
     const auto mr = gb_rows(a.mask + t0, a.mask ? rows : 0, 1);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int at = threadIdx.x + GX_THREADS * i, row = at / CPT, e = at % CPT * 4;
+      const int at = threadIdx.x + THREADS * i, row = at / CPT, e = at % CPT * 4;
       mask[i] = __builtin_amdgcn_raw_buffer_load_b8(mr, row, 0, 0);
       if constexpr (WHOLE) {
         const auto q = __builtin_amdgcn_raw_buffer_load_b128(sr, static_cast<int>(e < E ? row * pitch_s + e * 4 : GB_NOWHERE), 0, 0);
@@ -559,7 +554,7 @@ __global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxAr
   auto put = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int at = threadIdx.x + GX_THREADS * i, row = at / CPT, e = at % CPT * 4;
+      const int at = threadIdx.x + THREADS * i, row = at / CPT, e = at % CPT * 4;
       const bool real = !a.mask || mask[i];
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i][j] = real ? v[i][j] : 0.f;
@@ -567,8 +562,8 @@ __global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxAr
 #pragma unroll
       for (int u = 0; u < 2; ++u) gb_split(v[i][2 * u], v[i][2 * u + 1], q[0][u], q[1][u], q[2][u]);
 #pragma unroll
-      for (int p = 0; p < P; ++p) *reinterpret_cast<uint2*>(&pieces[buf][p][row * PITCH + e * 2]) = make_uint2(q[p][0], q[p][1]);
-      if (ACC && e == 0) reinterpret_cast<uint8_t*>(reals[buf])[row] = real;
+      for (int p = 0; p < P; ++p) *reinterpret_cast<uint2*>(lds + (buf * P + p) * PIECE + row * PITCH + e * 2) = make_uint2(q[p][0], q[p][1]);
+      if (ACC && e == 0) reinterpret_cast<uint8_t*>(reals + buf * (STEP / 4))[row] = real;
     }
   };
   load(begin);
@@ -589,31 +584,31 @@ __global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxAr
   // lane 16 g + c: tokens 4 g + 0..3 of every 16, its V columns
   const uint32_t at_out = col < d ? 4 * g * pitch + static_cast<uint32_t>(col) * B : GB_NOWHERE;
   int buf = 0;
-  for (uint32_t t0 = begin; t0 < end; t0 += GT, buf ^= 1) {
-    load(t0 + GT);                                   // behind the last step nothing is read
-    const int rows = min(static_cast<int>(end - t0), GT);
+  for (uint32_t t0 = begin; t0 < end; t0 += STEP, buf ^= 1) {
+    load(t0 + STEP);                                   // behind the last step nothing is read
+    const int rows = min(static_cast<int>(end - t0), STEP);
     const auto out = gb_rows(a.d_x + static_cast<int64_t>(t0) * pitch, rows, pitch);
 #pragma unroll
     for (int m = 0; m < GT / 16; ++m) {
       GbRow<BF16, V> old[ACC ? 4 : 1];
       if constexpr (ACC) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) old[r].load(out, at_out + (16 * m + r) * pitch);
+        for (int r = 0; r < 4; ++r) old[r].load(out, at_out + (first + 16 * m + r) * pitch);
       }
       gb_f32x4 acc[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) acc[i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        // lane 16 g + c: experts 32 k + 8 g + 0..7 of token 16 m + c
-        const int at = (16 * m + c) * PITCH + 64 * k + 16 * g;
+        // lane 16 g + c: experts 32 k + 8 g + 0..7 of token 16 m + c of this wave's
+        const int at = (first + 16 * m + c) * PITCH + 64 * k + 16 * g;
         uint4 q[P];
 #pragma unroll
-        for (int p = 0; p < P; ++p) q[p] = *reinterpret_cast<const uint4*>(&pieces[buf][p][at]);
+        for (int p = 0; p < P; ++p) q[p] = *reinterpret_cast<const uint4*>(lds + (buf * P + p) * PIECE + at);
         gb_products<BF16, BF16, V>(q[0], q[1], q[P - 1], w[k], acc);
       }
       uint32_t keep = 0x01010101u;                   // padded tokens: zeros, or nothing where d_x is added to
-      if constexpr (ACC) keep = reals[buf][4 * m + g];
+      if constexpr (ACC) keep = reals[buf * (STEP / 4) + first / 4 + 4 * m + g];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         GbRow<BF16, V> o;
@@ -629,11 +624,39 @@ __global__ __launch_bounds__(GX_THREADS, KS < 8 ? 2 : 1) void gate_x_kernel(GxAr
             o.w[i] = __float_as_uint(s);
           }
         }
-        o.store(out, keep >> (8 * r) & 1 ? at_out + (16 * m + r) * pitch : GB_NOWHERE);
+        o.store(out, keep >> (8 * r) & 1 ? at_out + (first + 16 * m + r) * pitch : GB_NOWHERE);
       }
     }
     put(buf ^ 1);
     __syncthreads();
+  }
+}
+
+// A launch of its own (launch_narrow says when 17 to 32 experts have one; more always do).
+template <bool BF16, int KS, int V, bool WHOLE, bool ACC>
+__global__ __launch_bounds__(256, KS < 8 ? 2 : 1) void gate_x_kernel(GxArgs a) {
+  using Tile = GxTile<BF16, KS, 256>;
+  __shared__ __align__(16) unsigned char lds[Tile::LDS];
+  __shared__ uint32_t reals[Tile::STEP / 2];
+  gate_x_block<BF16, KS, V, 256, WHOLE, ACC>(a, blockIdx.x, lds, reals);
+}
+
+// Up to 32 experts, where either gradient's blocks leave room for the other's: both in one launch, eight blocks of the one
+// and eight of the other in turn (one per XCD each), so that x is read while d_x is written.
+template <bool BF16, int MT, bool WHOLE, bool ACC>
+__global__ __launch_bounds__(GW_THREADS, MT == 1 && !ACC ? 4 : 2) void gate_narrow_kernel(GwArgs w, int blocks_w, GxArgs x, int blocks_x) {
+  constexpr int V = BF16 ? 8 : 4;
+  using Tile = GxTile<BF16, 1, GW_THREADS>;
+  __shared__ __align__(16) unsigned char lds[Tile::LDS > GW_LDS ? Tile::LDS : GW_LDS];
+  __shared__ float red_b[GW_WAVES][16 * MT];
+  __shared__ uint32_t reals[Tile::STEP / 2];
+  const int group = blockIdx.x / 8, both = min((blocks_w + 7) / 8, (blocks_x + 7) / 8);
+  const bool of_w = group < 2 * both ? group % 2 == 0 : blocks_w > blocks_x;
+  const int block = (group < 2 * both ? group / 2 : group - both) * 8 + blockIdx.x % 8;
+  if (of_w) {
+    if (block < blocks_w) gate_weight_block<BF16, MT, V>(w, block, lds, red_b);
+  } else {
+    if (block < blocks_x) gate_x_block<BF16, 1, V, GW_THREADS, WHOLE, ACC>(x, block, lds, reals);
   }
 }
 
@@ -668,76 +691,90 @@ size_t gate_backward_workspace_bytes(const moe_shape_t* shape) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * shape->E * (static_cast<size_t>(shape->d) + 1) * sizeof(float) : 0;
 }
 
-template <bool BF16> static int launch_weight(const GwPlan& p, const GwArgs& a, hipStream_t st) {
-  constexpr int V = BF16 ? 8 : 4;
-  const dim3 grid(static_cast<unsigned>(p.tiles * p.chunks * p.splits));
-  if (p.mt == 1) {
-    hipLaunchKernelGGL((gate_weight_kernel<BF16, 1, V>), grid, dim3(GW_THREADS), 0, st, a);
-  } else if (p.mt == 2) {
-    hipLaunchKernelGGL((gate_weight_kernel<BF16, 2, V>), grid, dim3(GW_THREADS), 0, st, a);
-  } else {
-    const auto kernel = gate_weight_wide_kernel<BF16, V>;
-    static LdsOnce once;
-    const int rc = ensure_dynamic_lds(once, reinterpret_cast<const void*>(kernel), GWW_LDS);
-    if (rc != MOE_OK) return rc;
-    hipLaunchKernelGGL(kernel, grid, dim3(GW_THREADS), GWW_LDS, st, a);
-  }
-  return MOE_OK;
-}
-
-template <bool BF16, int KS, int V> static void launch_x(GxArgs a, bool accumulate, hipStream_t st) {
-  constexpr int GT = GxTile<BF16, KS>::GT, COLS = 16 * V * GX_WAVES;
-  a.tiles = (a.d + COLS - 1) / COLS;
-  const int64_t most = (static_cast<int64_t>(a.T) + GT - 1) / GT;
-  int64_t n = 1024 / a.tiles;
+// Column tiles and parts of the tokens of the hidden states' gradient, for blocks of `step` tokens at a time.
+static GxArgs gx_plan(GxArgs a, int cols, int step, int most_blocks) {
+  a.tiles = (a.d + cols - 1) / cols;
+  const int64_t most = (static_cast<int64_t>(a.T) + step - 1) / step;
+  int64_t n = most_blocks / a.tiles;
   if (n > most) n = most;
   if (n > 8) n = n / 8 * 8;
   if (n < 1) n = 1;
-  int64_t per = (a.T + n - 1) / n;
-  per = (per + GT - 1) / GT * GT;
+  const int64_t per = (a.T + n - 1) / n;
   a.splits = static_cast<int>(n);
-  a.per_split = static_cast<int>(per);
-  const bool whole = a.E % 4 == 0;
+  a.per_split = static_cast<int>((per + step - 1) / step * step);
+  return a;
+}
+
+template <bool BF16, int KS> static void launch_x(GxArgs x, bool accumulate, hipStream_t st) {
+  constexpr int V = KS <= 2 ? (BF16 ? 8 : 4) : (BF16 ? 4 : 2);
+  x = gx_plan(x, 16 * V * GX_SIDE, GxTile<BF16, KS, 256>::STEP, 1024);
+  const bool whole = x.E % 4 == 0;
   const auto kernel = accumulate ? (whole ? gate_x_kernel<BF16, KS, V, true, true> : gate_x_kernel<BF16, KS, V, false, true>)
                                  : (whole ? gate_x_kernel<BF16, KS, V, true, false> : gate_x_kernel<BF16, KS, V, false, false>);
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(a.tiles * a.splits)), dim3(GX_THREADS), 0, st, a);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(x.tiles * x.splits)), dim3(256), 0, st, x);
+}
+
+// One launch for both gradients, but two for 17 to 32 experts beyond a round of blocks: their weights' blocks have a CU to
+// themselves, which costs the hidden states' more than the launch.  (Measured, one launch / two, us: E = 8, d = 4096, 501
+// tokens 14.0 / 16.5, 4096 18.8 / 19.3, 65536 234 / 238; E = 32, 2000 tokens, d = 2048 14.2 / 17.0; E = 24, 32768 tokens,
+// d = 4096 145 / 136.)
+template <bool BF16, int MT> static void launch_narrow(const GwArgs& w, const GxArgs& gx, bool with_w, bool with_x, bool accumulate, hipStream_t st) {
+  const GxArgs x = gx_plan(gx, 16 * (BF16 ? 8 : 4) * GX_SIDE, GxTile<BF16, 1, GW_THREADS>::STEP, 512);
+  const int blocks_w = with_w ? w.tiles * w.splits : 0;
+  int blocks_x = with_x ? x.tiles * x.splits : 0;
+  if (MT == 2 && blocks_w + blocks_x > 256 && with_x) {
+    launch_x<BF16, 1>(gx, accumulate, st);
+    blocks_x = 0;
+  }
+  const bool whole = x.E % 4 == 0;
+  const auto kernel = accumulate ? (whole ? gate_narrow_kernel<BF16, MT, true, true> : gate_narrow_kernel<BF16, MT, false, true>)
+                                 : (whole ? gate_narrow_kernel<BF16, MT, true, false> : gate_narrow_kernel<BF16, MT, false, false>);
+  const unsigned groups = static_cast<unsigned>((blocks_w + 7) / 8 + (blocks_x + 7) / 8);
+  if (groups > 0) hipLaunchKernelGGL(kernel, dim3(8 * groups), dim3(GW_THREADS), 0, st, w, blocks_w, x, blocks_x);
+}
+
+template <bool BF16> static int launch_wide(const GwArgs& w, hipStream_t st) {
+  const auto kernel = gate_weight_wide_kernel<BF16, BF16 ? 8 : 4>;
+  static LdsOnce once;
+  const int rc = ensure_dynamic_lds(once, reinterpret_cast<const void*>(kernel), GWW_LDS);
+  if (rc != MOE_OK) return rc;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(w.tiles * ((w.E + 63) / 64) * w.splits)), dim3(GW_THREADS), GWW_LDS, st, w);
+  return MOE_OK;
 }
 
 template <bool BF16>
-static void x_grad(const moe_shape_t* s, const void* w, const float* ds, const uint8_t* mask, bool accumulate, void* d_x, hipStream_t st) {
-  constexpr int V8 = BF16 ? 8 : 4, V4 = BF16 ? 4 : 2;
-  const GxArgs a = {static_cast<const char*>(w), ds, mask, static_cast<char*>(d_x), s->T, s->d, s->E, 0, 0, 0};
-  if (s->E <= 32)
-    launch_x<BF16, 1, V8>(a, accumulate, st);
-  else if (s->E <= 64)
-    launch_x<BF16, 2, V8>(a, accumulate, st);
-  else if (s->E <= 128)
-    launch_x<BF16, 4, V4>(a, accumulate, st);
-  else
-    launch_x<BF16, 8, V4>(a, accumulate, st);
-}
-
-template <bool BF16>
-static int gate_backward(const moe_shape_t* shape, const void* x, const void* w_gate, const float* d_scores, const uint8_t* mask,
+static int gate_backward(const moe_shape_t* s, const void* x, const void* w_gate, const float* d_scores, const uint8_t* mask,
                          float* d_w_gate, float* d_gate_bias, void* d_x, int accumulate, float* part, hipStream_t st) {
   const int acc_w = accumulate & MOE_ACCUMULATE_WEIGHTS ? 1 : 0, acc_x = accumulate & MOE_ACCUMULATE_X ? 1 : 0;
-  if (d_w_gate || d_gate_bias) {
-    const GwPlan p = gw_plan(shape);
-    const int64_t n = static_cast<int64_t>(shape->E) * shape->d;
-    const bool parts = p.splits > 1;
-    float* part_b = part + p.splits * n;
-    const GwArgs a = {static_cast<const char*>(x), d_scores, mask, d_w_gate ? (parts ? part : d_w_gate) : nullptr,
-                      d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, shape->T, shape->d, shape->E, p.tiles, p.splits, p.per_split, acc_w};
-    const int rc = launch_weight<BF16>(p, a, st);
-    if (rc != MOE_OK) return rc;
-    if (parts) {
-      const int blocks_w = d_w_gate ? static_cast<int>((n / 4 + GS_COLUMNS - 1) / GS_COLUMNS) : 0;
-      const int blocks_b = d_gate_bias ? (shape->E + GS_COLUMNS - 1) / GS_COLUMNS : 0;
-      hipLaunchKernelGGL(gate_sum_kernel, dim3(static_cast<unsigned>(blocks_w + blocks_b)), dim3(GS_THREADS), 0, st, part, d_w_gate, n,
-                         blocks_w, part_b, d_gate_bias, shape->E, p.splits, acc_w);
+  const bool with_w = d_w_gate || d_gate_bias, with_x = d_x && s->T > 0;
+  const GwPlan p = gw_plan(s);
+  const int64_t n = static_cast<int64_t>(s->E) * s->d;
+  const bool parts = p.splits > 1;
+  float* part_b = part + p.splits * n;
+  const GwArgs gw = {static_cast<const char*>(x), d_scores, mask, d_w_gate ? (parts ? part : d_w_gate) : nullptr,
+                     d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, s->T, s->d, s->E, p.tiles, p.splits, p.per_split, acc_w};
+  const GxArgs gx = {static_cast<const char*>(w_gate), d_scores, mask, static_cast<char*>(d_x), s->T, s->d, s->E, 0, 0, 0};
+  if (s->E <= 16) {
+    launch_narrow<BF16, 1>(gw, gx, with_w, with_x, acc_x, st);
+  } else if (s->E <= 32) {
+    launch_narrow<BF16, 2>(gw, gx, with_w, with_x, acc_x, st);
+  } else {
+    if (with_w) {
+      const int rc = launch_wide<BF16>(gw, st);
+      if (rc != MOE_OK) return rc;
+    }
+    if (with_x) {
+      if (s->E <= 64) launch_x<BF16, 2>(gx, acc_x, st);
+      else if (s->E <= 128) launch_x<BF16, 4>(gx, acc_x, st);
+      else launch_x<BF16, 8>(gx, acc_x, st);
     }
   }
-  if (d_x && shape->T > 0) x_grad<BF16>(shape, w_gate, d_scores, mask, acc_x, d_x, st);
+  if (with_w && parts) {
+    const int blocks_w = d_w_gate ? static_cast<int>((n / 4 + GS_COLUMNS - 1) / GS_COLUMNS) : 0;
+    const int blocks_b = d_gate_bias ? (s->E + GS_COLUMNS - 1) / GS_COLUMNS : 0;
+    hipLaunchKernelGGL(gate_sum_kernel, dim3(static_cast<unsigned>(blocks_w + blocks_b)), dim3(GS_THREADS), 0, st, part, d_w_gate, n,
+                       blocks_w, part_b, d_gate_bias, s->E, p.splits, acc_w);
+  }
   return launch_status();
 }
 
