@@ -575,7 +575,7 @@ extern "C" int moe_balance_loss(const moe_shape_t* shape, const float* scores, c
   if (!counts || !prob_sum || !loss || !workspace || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
   if (!aligned4(topk_idx) || !aligned4(counts) || !aligned4(prob_sum) || !aligned4(loss)) return MOE_ERR_INVALID_ARG;
   if (shape->T > 0 && (!scores || !topk_idx || !aligned16(scores))) return MOE_ERR_INVALID_ARG;
-  if (workspace_bytes < gate_loss_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
+  if (workspace_bytes < train_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E, k = shape->k;
   const GlPlan plan = gl_balance_plan(shape);
@@ -628,7 +628,7 @@ extern "C" int moe_gate_distill(const moe_shape_t* shape, const float* scores, c
   if (!loss || !workspace || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
   if (shape->T > 0 && (!scores || !target_scores || !aligned16(scores) || !aligned16(target_scores))) return MOE_ERR_INVALID_ARG;
   if (!aligned16(d_scores) || !aligned4(loss)) return MOE_ERR_INVALID_ARG;
-  if (workspace_bytes < gate_loss_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
+  if (workspace_bytes < train_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E;
   const GlPlan plan = gl_distill_plan(shape);

@@ -200,6 +200,9 @@ static int64_t grad_pieces(int32_t count, const moe_tensor_t* tensors, int64_t* 
   return pieces;
 }
 
+// One 64-bit sum per piece.
+static size_t grad_workspace_bytes(int64_t pieces) { return pieces > 0 ? (static_cast<size_t>(pieces) * 8 + 255) / 256 * 256 : 256; }
+
 // Calls launch(table, tensors in it, blocks) for up to GR_TENSORS tensors that have elements at a time.
 template <class F> static void for_tables(int32_t count, const moe_tensor_t* tensors, int64_t piece, F launch) {
   GradTable tab;
@@ -228,7 +231,7 @@ static int grads_call(int32_t count, const moe_tensor_t* tensors, bool clip, dou
   if (!norm || (reinterpret_cast<uintptr_t>(norm) & 3) || !workspace || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
   int64_t piece = 0;
   const int64_t pieces = grad_pieces(count, tensors, &piece);
-  if (workspace_bytes < static_cast<size_t>(pieces) * 8) return MOE_ERR_WORKSPACE;
+  if (workspace_bytes < grad_workspace_bytes(pieces)) return MOE_ERR_WORKSPACE;
   double* part = static_cast<double*>(workspace);
   int64_t at = 0;
   for_tables(count, tensors, piece, [&](const GradTable& tab, int n, int blocks) {
@@ -251,8 +254,7 @@ extern "C" int moe_grad_workspace_bytes(int32_t count, const moe_tensor_t* tenso
   if (rc != MOE_OK) return rc;
   if (!out_bytes) return MOE_ERR_INVALID_ARG;
   int64_t piece = 0;
-  *out_bytes = (static_cast<size_t>(moe::grad_pieces(count, tensors, &piece)) * 8 + 255) / 256 * 256;
-  if (*out_bytes == 0) *out_bytes = 256;
+  *out_bytes = moe::grad_workspace_bytes(moe::grad_pieces(count, tensors, &piece));
   return MOE_OK;
 }
 

@@ -26,9 +26,13 @@ inline int elem_bytes(int dtype) { return dtype == MOE_F32 ? 4 : 2; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// Workspace of the calls that train a gate; moe_train_workspace_bytes is the larger of the two.
+// What the calls that train a gate use of their workspace, and what moe_train_workspace_bytes asks for.
 size_t gate_loss_workspace_bytes(const moe_shape_t* shape);
 size_t gate_backward_workspace_bytes(const moe_shape_t* shape);
+inline size_t train_workspace_bytes(const moe_shape_t* shape) {
+  const size_t a = gate_loss_workspace_bytes(shape), b = gate_backward_workspace_bytes(shape), n = a > b ? a : b;
+  return n > 0 ? (n + 255) & ~static_cast<size_t>(255) : 256;
+}
 
 // Checks everything that does not depend on a particular call's pointers.
 inline int check_shape(const moe_shape_t* s) {

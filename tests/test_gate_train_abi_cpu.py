@@ -72,8 +72,8 @@ def test_workspaces():
     assert all(n >= 256 and n % 256 == 0 for n in sizes) and sizes[-1] < 2 ** 31
     nb = B.moe_train_workspace_bytes(SH)
     for call in (lambda: B.moe_balance_loss(SH, ONE, ONE, None, ONE, ONE, ONE, ONE, 16),
-                 lambda: B.moe_gate_distill(SH, ONE, ONE, None, 1.0, ONE, ONE, 0, ONE, 4),
-                 lambda: B.moe_gate_backward(B.make_shape(600, 128, 8, 2, 256, B.MOE_BF16, 1), ONE, ONE, ONE, None, ONE, None, None, 0, ONE, 16)):
+                 lambda: B.moe_gate_distill(SH, ONE, ONE, None, 1.0, ONE, ONE, 0, ONE, nb - 1),
+                 lambda: B.moe_gate_backward(SH, ONE, ONE, ONE, None, ONE, None, None, 0, ONE, nb - 1)):
         assert code_of(call) == -3
     assert nb < 1 << 24
     with pytest.raises(B.MoeError):
@@ -113,7 +113,7 @@ def test_norm_and_clip_refuse():
         assert code_of(lambda: call(lst, ONE + 2, ONE, BIG)) == -1
         assert code_of(lambda: call(lst, ONE, None, BIG)) == -1
         assert code_of(lambda: call(lst, ONE, ONE + 8, BIG)) == -1
-        assert code_of(lambda: call(lst, ONE, ONE, 4)) == -3
+        assert code_of(lambda: call(lst, ONE, ONE, 255)) == -3
     sizes = [B.moe_grad_workspace_bytes(raw_list(*[(ONE, ONE, n, 0)] * c)) for n, c in ((1, 1), (1, 3000), (2 ** 30, 4), (2 ** 40, 1))]
     assert all(nb % 256 == 0 for nb in sizes) and sizes[-1] <= 1 << 16
 
