@@ -143,7 +143,7 @@ struct GwArgs {
   const uint8_t* mask;
   float* out_w;
   float* out_b;
-  int T, d, E, tiles, splits, per_split, accumulate;
+  int T, d, E, tiles, chunks, splits, per_split, accumulate;
 };
 
 // The block's place: column tile, group of experts, part of the tokens.  All tiles and groups of a part are on one XCD
@@ -165,8 +165,8 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
   auto red = reinterpret_cast<gb_f32x4(*)[4][MOE_WAVE]>(lds);
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
   const int d = a.d, E = a.E, splits = a.splits;
-  const GwPlace at_block = gw_place(a.tiles, 1, splits, block);
-  const int tile = at_block.tile, split = at_block.split;
+  const GwPlace place = gw_place(a.tiles, a.chunks, splits, block);
+  const int tile = place.tile, split = place.split, e0 = place.chunk * 16 * MT;
   // (token numbers in 32 unsigned bits: T < 2^31, and no number passes it by more than the blocks' steps)
   const uint32_t begin = static_cast<uint32_t>(split) * a.per_split;
   const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
@@ -199,7 +199,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         ds[m][j] = gb_load_f32(gb_rows(s0 + j * pitch_s, left - j, pitch_s),
-                               8 * g * pitch_s + static_cast<uint32_t>(min(16 * m + c, E - 1)) * 4);
+                               8 * g * pitch_s + static_cast<uint32_t>(min(e0 + 16 * m + c, E - 1)) * 4);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j].load(gb_rows(x0 + static_cast<int64_t>(j) * pitch, with_w ? left - j : 0, pitch), at_x);
   };
@@ -252,7 +252,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
         for (int i = 0; i < 4; ++i) red[wave][i][lane] = acc[m][4 * quad + i];
         __syncthreads();
         const int cc = threadIdx.x & 15, row = threadIdx.x >> 4;
-        const int e = 16 * m + row, at = tile * 16 * V + V * cc + 4 * quad;
+        const int e = e0 + 16 * m + row, at = tile * 16 * V + V * cc + 4 * quad;
         if (row < 16 && e < E && at < d) {
           const int from = row / 4 * 16 + cc;
           float4* o = reinterpret_cast<float4*>(to + static_cast<int64_t>(e) * d + at);
@@ -277,7 +277,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
       if (g == 0) red_b[wave][16 * m + c] = v;
     }
     __syncthreads();
-    const int e = threadIdx.x;
+    const int e = e0 + threadIdx.x;
     if (threadIdx.x < 16 * MT && e < E) {
       float v = add ? a.out_b[e] : 0.f;
       for (int w = 0; w < GW_WAVES; ++w) v += red_b[w][threadIdx.x];
@@ -300,7 +300,7 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
   const int half = wave >> 2;
   const int d = a.d, E = a.E, splits = a.splits;
-  const GwPlace place = gw_place(a.tiles, (E + 63) / 64, splits, blockIdx.x);
+  const GwPlace place = gw_place(a.tiles, a.chunks, splits, blockIdx.x);
   const int e0 = place.chunk * 64;
   const uint32_t begin = static_cast<uint32_t>(place.split) * a.per_split;
   const uint32_t end = min(begin + a.per_split, static_cast<uint32_t>(a.T));
@@ -662,24 +662,32 @@ __global__ __launch_bounds__(GW_THREADS, MT == 1 && !ACC ? 4 : 2) void gate_narr
 
 // ------------------------------------------------------------------------------------------------ launches
 // Blocks of the weights' gradient: column tiles, groups of experts, and parts of the tokens, of which there are as many
-// as fill the chip (twice with up to 32 experts), each of a step of the block or more.  Small batches are one part: their
-// sums are stored at once, which saves a launch.  (Measured, one part / as many as fit, us: 501 tokens, d = 4096, E = 8
-// 10.8 / 14.1; 1000, d = 1048, E = 12 10.2 / 13.4; 100, d = 4096, E = 128 without d_x 11.6 / 13.7; but 200, d = 2048, E = 64
-// 20.7 / 17.5.)
+// as fill the chip (twice with 16 or 32 experts to a block), each of a step of the block or more.
+//
+// Up to 1024 tokens are one part, whose sums are stored at once: that saves a launch.  (Measured, one part / as many as
+// fit, us: d = 4096, 501 tokens, E = 8 10.8 / 14.1; 1000 tokens, E = 128 11.9 / 19.8; d = 1048, 1000 tokens, E = 12
+// 10.2 / 13.4.)
+//
+// More than 32 experts: blocks of 32 read x once for every 32, blocks of 64 are four times as wide and leave that many more
+// parts to be added up.  So the former take what is small, counted in bytes of x read.  (Measured, blocks of 32 / of 64,
+// us: d = 2048, E = 64, 2000 tokens 13 / 17, 8192 20 / 25, 16384 26 / 33, 32768 48 / 46, 65536 80 / 68; d = 4096, E = 128,
+// 1000 tokens 12 / 25, 2000 24 / 27, 4096 34 / 32, 8192 53 / 43; E = 256, 1000 tokens 16 / 27, 3000 43 / 35.)
 struct GwPlan {
   int mt, tiles, chunks, splits, per_split;
 };
 static GwPlan gw_plan(const moe_shape_t* s) {
   GwPlan p{};
-  p.mt = s->E <= 16 ? 1 : s->E <= 32 ? 2 : 4;
+  const int64_t x_reads = static_cast<int64_t>(s->T) * s->d * elem_bytes(s->dtype) * ((s->E + 31) / 32);
+  const bool wide = s->E > 32 && x_reads > (int64_t(s->E <= 64 ? 128 : 64) << 20);
+  p.mt = s->E <= 16 ? 1 : wide ? 4 : 2;
   const int v = s->dtype == MOE_F32 ? 4 : 8, cols = 16 * v * (p.mt == 4 ? 4 : 1);
   p.tiles = (s->d + cols - 1) / cols;
-  p.chunks = p.mt == 4 ? (s->E + 63) / 64 : 1;
+  p.chunks = (s->E + 16 * p.mt - 1) / (16 * p.mt);
   const int step = p.mt == 4 ? 64 : 32 * GW_WAVES;
   const int64_t most = (static_cast<int64_t>(s->T) + step - 1) / step;
   int64_t n = (p.mt == 4 ? 256 : 512) / (static_cast<int64_t>(p.tiles) * p.chunks);
   if (n > most) n = most;
-  if (s->T <= (p.mt == 4 ? 128 : 1024)) n = 1;
+  if (s->T <= 1024 && !wide) n = 1;
   if (n > 8) n = n / 8 * 8;
   if (n < 1) n = 1;
   int64_t per = (s->T + n - 1) / n;
@@ -724,7 +732,7 @@ template <bool BF16, int KS> static void launch_x(GxArgs x, bool accumulate, hip
 // d = 4096 145 / 136.)
 template <bool BF16, int MT> static void launch_narrow(const GwArgs& w, const GxArgs& gx, bool with_w, bool with_x, bool accumulate, hipStream_t st) {
   const GxArgs x = gx_plan(gx, 16 * (BF16 ? 8 : 4) * GX_SIDE, GxTile<BF16, 1, GW_THREADS>::STEP, 512);
-  const int blocks_w = with_w ? w.tiles * w.splits : 0;
+  const int blocks_w = with_w ? w.tiles * w.chunks * w.splits : 0;
   int blocks_x = with_x ? x.tiles * x.splits : 0;
   if (MT == 2 && blocks_w + blocks_x > 256 && with_x) {
     launch_x<BF16, 1>(gx, accumulate, st);
@@ -742,7 +750,7 @@ template <bool BF16> static int launch_wide(const GwArgs& w, hipStream_t st) {
   static LdsOnce once;
   const int rc = ensure_dynamic_lds(once, reinterpret_cast<const void*>(kernel), GWW_LDS);
   if (rc != MOE_OK) return rc;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(w.tiles * ((w.E + 63) / 64) * w.splits)), dim3(GW_THREADS), GWW_LDS, st, w);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(w.tiles * w.chunks * w.splits)), dim3(GW_THREADS), GWW_LDS, st, w);
   return MOE_OK;
 }
 
@@ -756,14 +764,16 @@ static int gate_backward(const moe_shape_t* s, const void* x, const void* w_gate
   const bool parts = p.splits > 1;
   float* part_b = part + p.splits * n;
   const GwArgs gw = {static_cast<const char*>(x), d_scores, mask, d_w_gate ? (parts ? part : d_w_gate) : nullptr,
-                     d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, s->T, s->d, s->E, p.tiles, p.splits, p.per_split, acc_w};
+                     d_gate_bias ? (parts ? part_b : d_gate_bias) : nullptr, s->T, s->d, s->E, p.tiles, p.chunks, p.splits, p.per_split, acc_w};
   const GxArgs gx = {static_cast<const char*>(w_gate), d_scores, mask, static_cast<char*>(d_x), s->T, s->d, s->E, 0, 0, 0};
   if (s->E <= 16) {
     launch_narrow<BF16, 1>(gw, gx, with_w, with_x, acc_x, st);
   } else if (s->E <= 32) {
     launch_narrow<BF16, 2>(gw, gx, with_w, with_x, acc_x, st);
   } else {
-    if (with_w) {
+    if (with_w && p.mt == 2) {
+      launch_narrow<BF16, 2>(gw, gx, true, false, false, st);
+    } else if (with_w) {
       const int rc = launch_wide<BF16>(gw, st);
       if (rc != MOE_OK) return rc;
     }

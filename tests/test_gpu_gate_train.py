@@ -313,10 +313,15 @@ def store(a, dtype):
     return a.astype(np.float32) if dtype == B.MOE_F32 else si.f32_to_bf16_bits(a.astype(np.float32))
 
 
-def check_gate(T, d, E, dtype, mask, seed, accumulate=0, parts="wbx", stream=None, scale=1.0):
+def check_gate(T, d, E, dtype, mask, seed, accumulate=0, parts="wbx", stream=None, scale=1.0, tokens=None):
+    """tokens: the only ones with a gradient; the sums over tokens then have that many terms, whatever T is."""
     rng = np.random.default_rng([seed, T, d, E])
     x, w = store(rng.standard_normal((T, d)), dtype), store(rng.standard_normal((E, d)) / np.sqrt(d), dtype)
     ds = (scale * rng.standard_normal((T, E)) * 10.0 ** rng.integers(-3, 1, (T, 1))).astype(np.float32)
+    if tokens is not None:
+        keep = np.zeros(T, dtype=bool)
+        keep[tokens] = True
+        ds[~keep] = 0.0
     nan = np.float32(np.nan) if dtype == B.MOE_F32 else np.uint16(0x7FC0)
     sh = shape_of(T, E, 1, 0, d, dtype)
     ws, nb = workspace(sh)
@@ -335,6 +340,7 @@ def check_gate(T, d, E, dtype, mask, seed, accumulate=0, parts="wbx", stream=Non
     rw, rb, rx = go.gate_backward(x64, w64, ds, mask)
     rw_size, rb_size, rx_size = go.gate_backward(np.abs(x64), np.abs(w64), np.abs(ds), mask)
     n = T if mask is None else int((mask != 0).sum())
+    n = n if tokens is None else len(tokens)
     where = f"T={T} d={d} E={E} dtype={dtype} accumulate={accumulate}"
     if "w" in parts:
         err, tol = np.abs(dw.np() - old[0] - rw), (n + 8) * 2 * U * rw_size + 2 * U * np.abs(old[0] + rw)
@@ -368,6 +374,16 @@ GATES = [(1, 8, 1), (1, 64, 8), (2, 16, 3), (3, 136, 16), (15, 120, 7), (16, 128
 def test_gate_backward(T, d, E, dtype):
     check_gate(T, d, E, dtype, None, 11)
     check_gate(T, d, E, dtype, mask_of("some", T, 11), 12, accumulate=3)
+
+
+@pytest.mark.parametrize("T,d,E,dtype", [(70001, 520, 8, 0), (70001, 264, 24, 1), (70001, 1048, 50, 1), (40001, 520, 64, 0), (33001, 1048, 65, 1),
+                                         (8200, 1048, 200, 1), (8201, 1048, 130, 0), (9001, 4096, 128, 1)])
+def test_gate_backward_of_large_batches(T, d, E, dtype):
+    """Blocks of 64 experts, several steps of a block, several parts; 60 tokens with a gradient, ends and edges among them."""
+    rng = np.random.default_rng([T, E])
+    tokens = np.unique(np.concatenate([[0, 1, 31, 32, 63, 64, 127, 128, T - 1, T - 2, T - 33, T - 64], rng.integers(0, T, 48)]))
+    check_gate(T, d, E, dtype, None, 16, tokens=tokens)
+    check_gate(T, d, E, dtype, mask_of("some", T, 16), 17, accumulate=3, tokens=tokens)
 
 
 @pytest.mark.parametrize("T,E", [(0, 8), (7, 8), (40, 24), (700, 64), (70, 256)])
