@@ -169,9 +169,24 @@ __device__ __forceinline__ void gl_rows(int T, int per_block, const uint8_t* __r
 // A block's row of sums in the workspace, whole 16-byte chunks.
 constexpr int gl_part_pitch(int E) { return (E + 3) / 4 * 4; }
 
-__device__ __forceinline__ float gl_balance_loss(double dot, double total, int E, int k) {
-  return total > 0.0 ? static_cast<float>(dot * E * k / (total * total)) : 0.f;
+// The loss from c_e and c_e P_e of expert e on thread e, 0 on threads without an expert.
+__device__ __forceinline__ void gl_finish_loss(double total, double dot, int E, int k, double (&lds)[2][MOE_MAX_E / MOE_WAVE], float* __restrict__ loss) {
+  const int wave = threadIdx.x / MOE_WAVE;
+  if (wave < MOE_MAX_E / MOE_WAVE) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+      total += __shfl_xor(total, off);
+      dot += __shfl_xor(dot, off);
+    }
+    if (lane_id() == 0) lds[0][wave] = total, lds[1][wave] = dot;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  total = (lds[0][0] + lds[0][1]) + (lds[0][2] + lds[0][3]);
+  dot = (lds[1][0] + lds[1][1]) + (lds[1][2] + lds[1][3]);
+  *loss = total > 0.0 ? static_cast<float>(dot * E * k / (total * total)) : 0.f;
 }
+static_assert(MOE_MAX_E == 4 * MOE_WAVE, "four waves of experts");
 
 // Counts and sums of a block's rows.  A single block finishes by itself (part_p is then not used), others leave a row of
 // the workspace each.
@@ -184,7 +199,7 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_kernel(const float* __
   constexpr int WAVES = GL_SUM_THREADS / MOE_WAVE;
   __shared__ float sum_p[WAVES][MOE_MAX_E];
   __shared__ int32_t cnt[MOE_MAX_E];
-  __shared__ double sums[WAVES];
+  __shared__ double sums[2][MOE_MAX_E / MOE_WAVE];
   const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, l = lane % G;
   if (threadIdx.x < MOE_MAX_E) cnt[threadIdx.x] = 0;
   __syncthreads();
@@ -235,13 +250,11 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_kernel(const float* __
     }
     return;
   }
-  const double total = gl_block_sum(static_cast<double>(c), sums);
-  const double dot = gl_block_sum(static_cast<double>(c) * v, sums);
   if (e < E) {
     counts[e] = c;
     prob_sum[e] = v;
   }
-  if (threadIdx.x == 0) *loss = gl_balance_loss(dot, total, E, k);
+  gl_finish_loss(static_cast<double>(c), static_cast<double>(c) * v, E, k, sums, loss);
 }
 
 // Adds the blocks' rows: L lanes of a wave (a power of two) for the experts of a row, four to a lane, so that a wave has
@@ -253,7 +266,7 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_finish_kernel(const fl
   constexpr int WAVES = GL_SUM_THREADS / MOE_WAVE;
   __shared__ double sp[WAVES][MOE_MAX_E];
   __shared__ int32_t sc[WAVES][MOE_MAX_E];
-  __shared__ double sums[WAVES];
+  __shared__ double sums[2][MOE_MAX_E / MOE_WAVE];
   const int lane = lane_id(), wave = threadIdx.x / MOE_WAVE, l = lane & (L - 1), pitch = gl_part_pitch(E);
   const int rows = GL_SUM_THREADS / L;
   double p[4] = {};
@@ -297,13 +310,11 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_finish_kernel(const fl
       sum += sp[w][e];
       count += sc[w][e];
     }
-  const double total = gl_block_sum(static_cast<double>(count), sums);
-  const double dot = gl_block_sum(count * sum, sums);
   if (e < E) {
     counts[e] = count;
     prob_sum[e] = static_cast<float>(sum);
   }
-  if (threadIdx.x == 0) *loss = gl_balance_loss(dot, total, E, k);
+  gl_finish_loss(static_cast<double>(count), count * sum, E, k, sums, loss);
 }
 
 // ds = gradient of sum_j d_topk_w[j] w_j (w: the routing weights of moe_route) + gradient of coef * L.
