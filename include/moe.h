@@ -322,6 +322,8 @@ int moe_place_replicas(int32_t E, const int32_t* loads, const int32_t* replicas,
  *               their gradients are 0; nothing else that belongs to them is used, whatever it holds.
  *   accumulate  gradients are added to what the output holds (a padded token's is then left as it was); 0: written
  *   T == 0      is valid: sums over tokens are written as 0 (or left, with accumulate)
+ *   outputs     must not overlap inputs, each other or the workspace (MOE_ERR_INVALID_ARG where d_scores, d_w_gate or
+ *               d_x overlaps a matrix or table that is read)
  *   workspace   16-byte aligned, contents ignored on entry and undefined on return; one buffer of
  *               moe_train_workspace_bytes() serves all calls of a shape that follow each other on a stream.  Calls that
  *               share a workspace must not overlap in time (replays of captured graphs are calls).
@@ -374,7 +376,7 @@ int moe_gate_distill(const moe_shape_t* shape, const float* scores, const float*
  *   d_x[t,:]       = sum_e d_scores[t,e] w_gate[e,:]     [T,d] in `dtype`, or NULL; rounded once
  * At least one of them.  x is used for d_w_gate only, w_gate for d_x only (else they may be NULL), the workspace for
  * d_w_gate and d_gate_bias.  accumulate: 0, or a sum of MOE_ACCUMULATE_WEIGHTS (d_w_gate and d_gate_bias: micro-batches)
- * and MOE_ACCUMULATE_X (d_x: next to what the experts' gradients left there).  Rows of x of at most 32 MiB (else
+ * and MOE_ACCUMULATE_X (d_x: next to what the experts' gradients left there).  Rows of x of at most 16 MiB (else
  * MOE_ERR_UNSUPPORTED).
  */
 #define MOE_ACCUMULATE_WEIGHTS 1
@@ -387,8 +389,8 @@ int moe_gate_backward(const moe_shape_t* shape, const void* x, const void* w_gat
  * Global gradient norm and clipping over a list of tensors (the gradients of all gates of a model, say):
  *   norm = sqrt(sum over all elements of all tensors of g^2), in 64 bits, stored as fp32 [1]
  *   out  = g * c, one product and one rounding;  c = max_norm / norm if norm > max_norm, else 1
- * If norm is not finite (an infinity or NaN among the gradients) c is 1: the caller finds it in `norm` and skips the
- * step.  `tensors` is a HOST array, read before the call returns.  Tensors are contiguous; data and out need no more
+ * If norm is not finite (an infinity or NaN among the gradients, or a norm beyond fp32) c is 1: the caller finds it in
+ * `norm` and skips the step.  `tensors` is a HOST array, read before the call returns.  Tensors are contiguous; data and out need no more
  * than their elements' alignment; `out` may be `data` (in place; nothing is written then if c is 1), but must not
  * overlap the tensors otherwise, and no two outputs may overlap.  `out` is not used by moe_grad_norm.  n == 0 and
  * count == 0 are valid.  max_norm: not negative, infinity allowed.  At most 2^40 elements.  workspace: as above, at

@@ -252,7 +252,7 @@ def moe_place_replicas(E, loads, replicas, n_gpus, prev_replicas, prev_gpu, gpu_
 
 # ---- training a gate.  Tensors given to these calls are checked here (type, size, contiguity, the current GPU), as a
 # ---- mask or a gradient of another size would be read out of range; plain device addresses (int) are taken as they are.
-_F32, _I32, _MASK, _BYTES = "f32", "i32", "mask", "bytes"
+F32, I32, MASK, BYTES = "f32", "i32", "mask", "bytes"
 _types = _current_gpu = None
 
 
@@ -262,12 +262,12 @@ def _tensor_types():
     if _types is None:
         import torch
         _current_gpu = torch.cuda.current_device
-        _types = {_F32: (torch.float32,), _I32: (torch.int32,), _MASK: (torch.bool, torch.uint8),
-                  _BYTES: (torch.uint8, torch.int8), MOE_F32: (torch.float32,), MOE_BF16: (torch.bfloat16,)}
+        _types = {F32: (torch.float32,), I32: (torch.int32,), MASK: (torch.bool, torch.uint8),
+                  BYTES: (torch.uint8, torch.int8), MOE_F32: (torch.float32,), MOE_BF16: (torch.bfloat16,)}
     return _types
 
 
-def _addresses(call, *operands):
+def check_tensors(call, *operands):
     """Device addresses of (name, tensor or address or None, kind, elements) operands, after their checks.  A buffer of
     bytes may be larger than asked for."""
     out, gpu, types = [], None, None
@@ -281,7 +281,7 @@ def _addresses(call, *operands):
                 gpu = _current_gpu()
         have = t.numel()
         if t.get_device() == gpu and t.dtype in types[kind] and t.is_contiguous() and \
-                (have == numel or have > numel and kind is _BYTES):
+                (have == numel or have > numel and kind is BYTES):
             out.append(t.data_ptr())
             continue
         want = " or ".join(map(str, types[kind]))
@@ -300,18 +300,18 @@ def moe_train_workspace_bytes(shape: MoeShape) -> int:
 def moe_balance_loss(shape, scores, topk_idx, token_mask, counts, prob_sum, loss, workspace,
                      workspace_bytes, stream=None):
     T, E, k, nb = shape.T, shape.E, shape.k, int(workspace_bytes)
-    a = _addresses("moe_balance_loss", ("scores", scores, _F32, T * E), ("topk_idx", topk_idx, _I32, T * k),
-                   ("token_mask", token_mask, _MASK, T), ("counts", counts, _I32, E),
-                   ("prob_sum", prob_sum, _F32, E), ("loss", loss, _F32, 1), ("workspace", workspace, _BYTES, nb))
+    a = check_tensors("moe_balance_loss", ("scores", scores, F32, T * E), ("topk_idx", topk_idx, I32, T * k),
+                   ("token_mask", token_mask, MASK, T), ("counts", counts, I32, E),
+                   ("prob_sum", prob_sum, F32, E), ("loss", loss, F32, 1), ("workspace", workspace, BYTES, nb))
     _check("moe_balance_loss", load().moe_balance_loss(ctypes.byref(shape), *a, nb, _stream(stream)))
 
 
 def moe_route_backward(shape, scores, topk_idx, d_topk_w, counts, balance_coef, token_mask, d_scores,
                        accumulate=0, stream=None):
     T, E, k = shape.T, shape.E, shape.k
-    a = _addresses("moe_route_backward", ("scores", scores, _F32, T * E), ("topk_idx", topk_idx, _I32, T * k),
-                   ("d_topk_w", d_topk_w, _F32, T * k), ("counts", counts, _I32, E),
-                   ("token_mask", token_mask, _MASK, T), ("d_scores", d_scores, _F32, T * E))
+    a = check_tensors("moe_route_backward", ("scores", scores, F32, T * E), ("topk_idx", topk_idx, I32, T * k),
+                   ("d_topk_w", d_topk_w, F32, T * k), ("counts", counts, I32, E),
+                   ("token_mask", token_mask, MASK, T), ("d_scores", d_scores, F32, T * E))
     _check("moe_route_backward",
            load().moe_route_backward(ctypes.byref(shape), *a[:4], float(balance_coef), *a[4:], int(accumulate),
                                      _stream(stream)))
@@ -320,9 +320,9 @@ def moe_route_backward(shape, scores, topk_idx, d_topk_w, counts, balance_coef, 
 def moe_gate_distill(shape, scores, target_scores, token_mask, coef, loss, d_scores, accumulate,
                      workspace, workspace_bytes, stream=None):
     T, E, nb = shape.T, shape.E, int(workspace_bytes)
-    a = _addresses("moe_gate_distill", ("scores", scores, _F32, T * E), ("target_scores", target_scores, _F32, T * E),
-                   ("token_mask", token_mask, _MASK, T), ("loss", loss, _F32, 1), ("d_scores", d_scores, _F32, T * E),
-                   ("workspace", workspace, _BYTES, nb))
+    a = check_tensors("moe_gate_distill", ("scores", scores, F32, T * E), ("target_scores", target_scores, F32, T * E),
+                   ("token_mask", token_mask, MASK, T), ("loss", loss, F32, 1), ("d_scores", d_scores, F32, T * E),
+                   ("workspace", workspace, BYTES, nb))
     _check("moe_gate_distill",
            load().moe_gate_distill(ctypes.byref(shape), *a[:3], float(coef), *a[3:5], int(accumulate), a[5], nb,
                                    _stream(stream)))
@@ -331,10 +331,10 @@ def moe_gate_distill(shape, scores, target_scores, token_mask, coef, loss, d_sco
 def moe_gate_backward(shape, x, w_gate, d_scores, token_mask, d_w_gate, d_gate_bias, d_x, accumulate,
                       workspace, workspace_bytes, stream=None):
     T, d, E, nb = shape.T, shape.d, shape.E, int(workspace_bytes)
-    a = _addresses("moe_gate_backward", ("x", x, shape.dtype, T * d), ("w_gate", w_gate, shape.dtype, E * d),
-                   ("d_scores", d_scores, _F32, T * E), ("token_mask", token_mask, _MASK, T),
-                   ("d_w_gate", d_w_gate, _F32, E * d), ("d_gate_bias", d_gate_bias, _F32, E),
-                   ("d_x", d_x, shape.dtype, T * d), ("workspace", workspace, _BYTES, nb))
+    a = check_tensors("moe_gate_backward", ("x", x, shape.dtype, T * d), ("w_gate", w_gate, shape.dtype, E * d),
+                   ("d_scores", d_scores, F32, T * E), ("token_mask", token_mask, MASK, T),
+                   ("d_w_gate", d_w_gate, F32, E * d), ("d_gate_bias", d_gate_bias, F32, E),
+                   ("d_x", d_x, shape.dtype, T * d), ("workspace", workspace, BYTES, nb))
     _check("moe_gate_backward",
            load().moe_gate_backward(ctypes.byref(shape), *a[:7], int(accumulate), a[7], nb, _stream(stream)))
 
@@ -352,7 +352,7 @@ class GradList:
         spans = []
         for i, (g, o) in enumerate(zip(self.grads, self.out)):
             dtype = MOE_BF16 if g.dtype in _tensor_types()[MOE_BF16] else MOE_F32
-            data, out = _addresses("GradList", (f"gradient {i}", g, dtype, g.numel()), (f"output {i}", o, dtype, g.numel()))
+            data, out = check_tensors("GradList", (f"gradient {i}", g, dtype, g.numel()), (f"output {i}", o, dtype, g.numel()))
             self.array[i] = MoeTensor(data, out, g.numel(), dtype, 0)
             nbytes = g.numel() * g.element_size()
             if nbytes:
@@ -381,11 +381,11 @@ def moe_grad_workspace_bytes(grads: GradList) -> int:
 
 def moe_grad_norm(grads: GradList, norm, workspace, workspace_bytes, stream=None):
     nb = int(workspace_bytes)
-    a = _addresses("moe_grad_norm", ("norm", norm, _F32, 1), ("workspace", workspace, _BYTES, nb))
+    a = check_tensors("moe_grad_norm", ("norm", norm, F32, 1), ("workspace", workspace, BYTES, nb))
     _check("moe_grad_norm", load().moe_grad_norm(len(grads), grads.array, *a, nb, _stream(stream)))
 
 
 def moe_clip_grads(grads: GradList, max_norm, norm, workspace, workspace_bytes, stream=None):
     nb = int(workspace_bytes)
-    a = _addresses("moe_clip_grads", ("norm", norm, _F32, 1), ("workspace", workspace, _BYTES, nb))
+    a = check_tensors("moe_clip_grads", ("norm", norm, F32, 1), ("workspace", workspace, BYTES, nb))
     _check("moe_clip_grads", load().moe_clip_grads(len(grads), grads.array, float(max_norm), *a, nb, _stream(stream)))

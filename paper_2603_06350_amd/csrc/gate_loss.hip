@@ -615,6 +615,9 @@ extern "C" int moe_route_backward(const moe_shape_t* shape, const float* scores,
   if (!scores || !d_scores || (d_topk_w && !topk_idx)) return MOE_ERR_INVALID_ARG;
   if (!aligned16(scores) || !aligned16(d_scores) || !aligned4(topk_idx) || !aligned4(d_topk_w) || !aligned4(counts))
     return MOE_ERR_INVALID_ARG;
+  const int64_t table = int64_t(4) * shape->T * shape->E, choices = int64_t(4) * shape->T * shape->k;
+  if (!apart(d_scores, table, scores, table) || !apart(d_scores, table, d_topk_w, choices) || !apart(d_scores, table, topk_idx, choices))
+    return MOE_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E, k = shape->k;
   const GlPlan plan = gl_route_plan(shape);
@@ -640,6 +643,8 @@ extern "C" int moe_gate_distill(const moe_shape_t* shape, const float* scores, c
   if (shape->T > 0 && (!scores || !target_scores || !aligned16(scores) || !aligned16(target_scores))) return MOE_ERR_INVALID_ARG;
   if (!aligned16(d_scores) || !aligned4(loss)) return MOE_ERR_INVALID_ARG;
   if (workspace_bytes < train_workspace_bytes(shape)) return MOE_ERR_WORKSPACE;
+  const int64_t table = int64_t(4) * shape->T * shape->E;
+  if (!apart(d_scores, table, scores, table) || !apart(d_scores, table, target_scores, table)) return MOE_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int T = shape->T, E = shape->E;
   const GlPlan plan = gl_distill_plan(shape);

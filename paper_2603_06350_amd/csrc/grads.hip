@@ -158,8 +158,8 @@ __global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, i
   __shared__ double lds[GR_THREADS / MOE_WAVE];
   const double s = grad_total_norm(part, pieces, lds);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(s);
-  // 1 where the norm is no finite number: the caller sees it in `norm`
-  const float c = s > max_norm && s < INFINITY ? static_cast<float>(max_norm / s) : 1.f;
+  // 1 where `norm`, which the caller sees, is no finite number
+  const float c = s > max_norm && static_cast<float>(s) < INFINITY ? static_cast<float>(max_norm / s) : 1.f;
   const int b = (gridDim.x / 8 - 1 - blockIdx.x / 8) * 8 + blockIdx.x % 8;
   if (b >= blocks) return;
   const GradPiece g = grad_piece(tab, count, piece, b);

@@ -25,6 +25,11 @@ inline int elem_bytes(int dtype) { return dtype == MOE_F32 ? 4 : 2; }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// No byte in common; NULL has none.
+inline bool apart(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+  return !a || !b || pa + bytes_a <= pb || pb + bytes_b <= pa;
+}
 
 // What the calls that train a gate use of their workspace, and what moe_train_workspace_bytes asks for.
 size_t gate_loss_workspace_bytes(const moe_shape_t* shape);

@@ -192,8 +192,10 @@ class GateTrainer:
     def score(self, x, w_gate, scores, gate_bias=None, stream=None):
         """The scores [T, E] of a gate on x: targets for the gates that predict it."""
         s = torch.cuda.current_stream() if stream is None else stream
-        B.moe_route_ws(self.shape, x, w_gate, gate_bias, self.topk_idx, self.topk_w, scores, self.workspace,
-                       self.ws_bytes, s)
+        sh = self.shape
+        B.check_tensors("GateTrainer.score", ("x", x, sh.dtype, sh.T * sh.d), ("w_gate", w_gate, sh.dtype, sh.E * sh.d),
+                        ("scores", scores, B.F32, sh.T * sh.E), ("gate_bias", gate_bias, B.F32, sh.E))
+        B.moe_route_ws(sh, x, w_gate, gate_bias, self.topk_idx, self.topk_w, scores, self.workspace, self.ws_bytes, s)
 
     def enqueue(self, i, x, w_gate, target_scores, gate_bias=None, token_mask=None, accumulate=False, d_x=None,
                 stream=None):
@@ -222,6 +224,7 @@ class GateTrainer:
 def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps, lr, token_mask=None):
     """Fine-tunes gate 0 of `trainer`, starting from w_gate: predictor of `target_scores` from x_now.  Returns the new
     weights in w_gate's type and the losses of the steps.  The optimizer is PyTorch's Adam on an fp32 copy."""
+    w_gate = w_gate.detach()
     master = w_gate.float().clone().requires_grad_(True)
     opt = torch.optim.Adam([master], lr=lr)
     w, losses = w_gate.clone(), []

@@ -9,6 +9,16 @@ ONE = 0x1000          # an aligned address that no case below gets to use
 BIG = 1 << 40
 
 
+def addresses(*there):
+    """Addresses far enough from each other for one argument each; None for those that are not there."""
+    return [ONE + (i + 1) * (1 << 36) if t else None for i, t in enumerate(there)]
+
+
+def put(args, i, a):
+    """Argument i: None, a small number, or its own address moved by as much as a differs from ONE."""
+    args[i] = args[i] + a - ONE if a is not None and a >= ONE else a
+
+
 @pytest.fixture(scope="module", autouse=True)
 def _lib():
     if not os.path.exists(B.lib_path()):
@@ -29,16 +39,17 @@ SH = B.make_shape(64, 128, 8, 2, 256, B.MOE_BF16, 1)
 @pytest.mark.parametrize("i,a", [(0, None), (1, None), (3, None), (4, None), (5, None), (6, None), (0, ONE + 4), (1, ONE + 2),
                                  (3, ONE + 1), (4, ONE + 2), (5, ONE + 2), (6, ONE + 8)])
 def test_balance_loss_refuses(i, a):
-    args = [ONE, ONE, None, ONE, ONE, ONE, ONE]
-    args[i] = a
+    args = addresses(1, 1, 1, 1, 1, 1, 1)
+    put(args, i, a)
     assert code_of(lambda: B.moe_balance_loss(SH, *args, BIG)) == -1
 
 
 @pytest.mark.parametrize("i,a", [(0, None), (1, None), (6, None), (0, ONE + 4), (1, ONE + 2), (2, ONE + 2), (3, ONE + 2), (6, ONE + 8),
                                  (7, 2), (7, -1)])
 def test_route_backward_refuses(i, a):
-    args = [ONE, ONE, ONE, ONE, 1.0, None, ONE, 0]
-    args[i] = a
+    args = addresses(1, 1, 1, 1, 1, 0, 1, 1)
+    args[4], args[7] = 1.0, 0
+    put(args, i, a)
     assert code_of(lambda: B.moe_route_backward(SH, *args)) == -1
 
 
@@ -49,17 +60,45 @@ def test_route_backward_needs_one_of_its_parts():
 @pytest.mark.parametrize("i,a", [(0, None), (1, None), (4, None), (7, None), (0, ONE + 4), (1, ONE + 4), (4, ONE + 1), (5, ONE + 4), (6, 2),
                                  (7, ONE + 4)])
 def test_gate_distill_refuses(i, a):
-    args = [ONE, ONE, None, 1.0, ONE, ONE, 0, ONE]
-    args[i] = a
+    args = addresses(1, 1, 0, 1, 1, 1, 1, 1)
+    args[3], args[6] = 1.0, 0
+    put(args, i, a)
     assert code_of(lambda: B.moe_gate_distill(SH, *args, BIG)) == -1
 
 
 @pytest.mark.parametrize("i,a", [(0, None), (1, None), (2, None), (8, None), (0, ONE + 8), (1, ONE + 8), (2, ONE + 8), (4, ONE + 8), (5, ONE + 2),
                                  (6, ONE + 8), (7, 4), (7, -1), (8, ONE + 8)])
 def test_gate_backward_refuses(i, a):
-    args = [ONE, ONE, ONE, None, ONE, ONE, ONE, 0, ONE]
-    args[i] = a
+    args = addresses(1, 1, 1, 0, 1, 1, 1, 1, 1)
+    args[7] = 0
+    put(args, i, a)
     assert code_of(lambda: B.moe_gate_backward(SH, *args, BIG)) == -1
+
+
+@pytest.mark.parametrize("inside", [0, 16])
+@pytest.mark.parametrize("out,read", [("d_x", "x"), ("d_x", "w_gate"), ("d_x", "d_scores"), ("d_w_gate", "x"), ("d_w_gate", "w_gate"),
+                                      ("d_w_gate", "d_scores"), ("d_w_gate", "d_x")])
+def test_gate_backward_refuses_outputs_that_are_read(out, read, inside):
+    names = ("x", "w_gate", "d_scores", "mask", "d_w_gate", "d_gate_bias", "d_x", "accumulate", "workspace")
+    args = dict(zip(names, addresses(1, 1, 1, 0, 1, 1, 1, 1, 1)), accumulate=0)
+    args[out] = args[read] + inside
+    assert code_of(lambda: B.moe_gate_backward(SH, *args.values(), BIG)) == -1
+
+
+@pytest.mark.parametrize("inside", [-16, 0, 16])
+def test_score_gradients_are_not_written_over_what_is_read(inside):
+    scores, idx, dw, counts, target, loss, ws = addresses(1, 1, 1, 1, 1, 1, 1)
+    for read in (scores, dw, idx):
+        assert code_of(lambda: B.moe_route_backward(SH, scores, idx, dw, counts, 1.0, None, read + inside)) == -1
+    for read in (scores, target):
+        assert code_of(lambda: B.moe_gate_distill(SH, scores, target, None, 1.0, loss, read + inside, 0, ws, BIG)) == -1
+
+
+@pytest.mark.parametrize("dtype,d", [(B.MOE_BF16, 2 ** 23 + 8), (B.MOE_F32, 2 ** 22 + 4), (B.MOE_BF16, 2 ** 24)])
+def test_gate_backward_refuses_rows_that_its_offsets_do_not_reach(dtype, d):
+    args = addresses(1, 1, 1, 0, 1, 1, 1, 1, 1)
+    args[7] = 0
+    assert code_of(lambda: B.moe_gate_backward(B.make_shape(2, d, 2, 1, 8, dtype, 0), *args, BIG)) == -2
 
 
 def test_gate_backward_needs_an_output():

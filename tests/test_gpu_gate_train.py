@@ -405,6 +405,30 @@ def test_gate_backward_of_gradients_of_any_size(scale, dtype):
 
 
 # ------------------------------------------------------------------------------------------------ norm and clipping
+@pytest.mark.parametrize("E", [2, 24, 40])
+def test_gate_backward_of_the_longest_rows(E):
+    """Rows of 16 MiB; columns at both ends and in between against 64 bits, tolerances as in check_gate."""
+    T, d, n = 130, 2 ** 23, 512
+    gen = torch.Generator(device="cuda").manual_seed(E)
+    x = torch.empty((T, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    w = torch.empty((E, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    ds = torch.empty((T, E), device="cuda").normal_(generator=gen)
+    dw, db = torch.full((E, d), -77.0, device="cuda"), torch.full((E,), -77.0, device="cuda")
+    dx = torch.full((T, d), -77.0, dtype=torch.bfloat16, device="cuda")
+    sh = shape_of(T, E, 1, 0, d)
+    ws, nb = workspace(sh)
+    B.moe_gate_backward(sh, x, w, ds, None, dw, db, dx, 0, ws, nb)
+    at = torch.cat([torch.arange(n), torch.randint(0, d, (n,), generator=torch.Generator().manual_seed(1)), torch.arange(d - n, d)]).cuda()
+    x64, w64, ds64 = (t.double().cpu().numpy() for t in (x[:, at], w[:, at], ds))
+    rw, rb, rx = go.gate_backward(x64, w64, ds64)
+    rw_size, rb_size, rx_size = go.gate_backward(np.abs(x64), np.abs(w64), np.abs(ds64))
+    assert (np.abs(dw[:, at].double().cpu().numpy() - rw) <= (T + 8) * 2 * U * rw_size + 2 * U * np.abs(rw)).all()
+    assert (np.abs(db.double().cpu().numpy() - rb) <= (T + 8) * 2 * U * rb_size + 2 * U * np.abs(rb)).all()
+    half = 2.0 ** -8
+    tol = half * np.abs(rx) + (1 + half) * ((E + 8) * 2 * U + 2.0 ** -16) * rx_size
+    assert (np.abs(dx[:, at].double().cpu().numpy() - rx) <= tol).all()
+
+
 def make_grads(sizes, seed, kinds="fb", offset=0):
     """Tensors of the given sizes, alternately fp32 and bf16, each starting `offset` elements into its allocation."""
     rng = np.random.default_rng([seed, len(sizes)])
@@ -489,6 +513,15 @@ def test_gradients_that_are_not_finite_are_left_and_reported(bad):
     assert not np.isfinite(float(norm))
     for a, b in zip(g, out):
         assert torch.equal(torch.nan_to_num(a.float(), 5.0), torch.nan_to_num(b.float(), 5.0))
+
+
+def test_a_norm_beyond_fp32_leaves_the_gradients():
+    g = [torch.full((4,), 3e38, device="cuda"), torch.ones(9, device="cuda")]
+    lst = B.GradList(g, [torch.zeros_like(t) for t in g])
+    nb = B.moe_grad_workspace_bytes(lst)
+    ws, norm = torch.empty(nb, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+    B.moe_clip_grads(lst, 1.0, norm, ws, nb)
+    assert np.isinf(float(norm)) and all(torch.equal(a, b) for a, b in zip(g, lst.out))
 
 
 # ------------------------------------------------------------------------------------------------ as they are used
@@ -640,6 +673,24 @@ def test_finetuning_runs():
     pred, true, kept = layer.predicted_vs_actual_loads(test, x, x, new, w_later=w)
     assert pred.sum() == true.sum() == T * k and 0.0 <= kept <= 1.0
     assert layer.predicted_vs_actual_loads(test, x, x, w)[2] == 1.0
+
+
+def test_trainer_takes_nothing_that_does_not_fit():
+    T, d, E = 32, 64, 8
+    tr = layer.GateTrainer(T, d, E, 2, 1, B.MOE_BF16, 1)
+    f = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype, device="cuda")          # noqa: E731
+    x, w, target = f(T, d), f(E, d), f(T, E, dtype=torch.float32)
+    for args, kw in (((0, x[:T - 1], w, target), {}), ((0, x, w.float(), target), {}), ((0, x, f(d, E).t(), target), {}),
+                     ((0, x, w, target[:, :E - 1]), {}), ((1, x, w, target), {}), ((0, x, w, target), dict(gate_bias=f(E))),
+                     ((0, x, w, target), dict(token_mask=f(T - 1, dtype=torch.bool))), ((0, x, w, target), dict(d_x=f(T, d + 8)))):
+        with pytest.raises(ValueError):
+            tr.enqueue(*args, **kw)
+    with pytest.raises(B.MoeError):
+        tr.enqueue(0, x, w, target, d_x=x)
+    # a gate that is part of a model: its own gradient is not touched
+    model = w.clone().requires_grad_(True)
+    new, _ = layer.finetune_predictor(tr, x, target, model, 1, 1e-3)
+    assert not new.requires_grad and model.grad is None
 
 
 def test_an_empty_batch_gives_zeros_or_leaves_what_is_there():
