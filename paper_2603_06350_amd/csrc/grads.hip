@@ -1,6 +1,8 @@
 // moe_grad_norm, moe_clip_grads: the Euclidean norm of a list of tensors taken together, and the tensors scaled to a
 // largest norm:  norm = sqrt(sum over all elements of g^2),  out = g * min(1, max_norm / norm).
-// HBM-bound: every element is read once for the norm, and once more with a write for the scaling.
+// HBM-bound: every element is read once for the norm, and once more with a write for the scaling.  (Measured: 60 tensors
+// of 5 to 14336 x 4096 elements, 844 MB of fp32 and bf16, 459 us, of it the norm 143 = 5.9 TB/s and the scaling 310 =
+// 5.4 TB/s read and written; 32 tensors of 512 KiB 11.6 us.)
 //
 // The list travels in the kernels' arguments, so no table has to reach the device first and a captured graph holds its
 // own copy.  Every block takes one piece of one tensor.  Squares and their sums are 64-bit (an fp32 square overflows
@@ -12,8 +14,12 @@ namespace moe {
 
 constexpr int GR_THREADS = 256;
 constexpr int GR_TENSORS = 128;        // tensors of one launch
-constexpr int64_t GR_PIECE = 8192;     // least elements of a piece; all pieces of a call have the same size
-constexpr int64_t GR_PIECES = 4096;    // pieces of a call that is large enough
+// Least elements of a piece (all pieces of a call have the same size), and the pieces of a call that is large enough: small
+// pieces fill the chip, few of them are less to add up, which every block does.  (Measured, pieces of 4096 / 8192 / 16384,
+// us: one tensor of 100000 5.9 / 6.4 / 7.1, 32 of 131072 12.4 / 11.6 / 11.5, 40 of up to 2000000 22.9 / 20.8 / 20.4.
+// 2048 / 4096 / 8192 pieces: 844 MB 470 / 459 / 446, 512 MiB of bf16 282 / 281 / 288.)
+constexpr int64_t GR_PIECE = 8192;
+constexpr int64_t GR_PIECES = 4096;
 
 struct GradTable {
   const void* data[GR_TENSORS];
@@ -152,7 +158,8 @@ template <bool BF16> __device__ __forceinline__ void grad_scale(const GradPiece&
 
 // Every block makes the factor from the pieces' sums by itself, which saves a launch.  The pieces are taken from the last
 // eight to the first: what the norm's pass read last is in the memory-side cache, and in the L2 of the XCD that block b
-// of both passes runs on (b % 8).  The grid is a multiple of 8.
+// of both passes runs on (b % 8).  The grid is a multiple of 8.  (Measured, first to last / last to first, us: 844 MB 486 /
+// 459, 512 MiB of bf16 301 / 281.  What is written is not read soon and goes past the L2: with ordinary stores 490, 312.)
 __global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, int count, int blocks, int64_t piece, const double* __restrict__ part,
                                                                 int64_t pieces, double max_norm, float* __restrict__ norm) {
   __shared__ double lds[GR_THREADS / MOE_WAVE];
