@@ -6,7 +6,7 @@
 // All three stream tables of T x E floats once: HBM-bound for large batches, launch-bound for small ones.  (Measured, in a
 // queue that is kept full, 65536 tokens: distill with a gradient, 128 experts 100 MB in 20.7 us = 4.9 TB/s and 27 with
 // the mask's count and the sum of the loss; balance and its gradient, 64 experts 21 us in three launches, 52 MB; route
-// backward, 128 experts 24.7 us, 71 MB.  A single small call takes 4 to 6 us.)
+// backward, 128 experts, k = 8 18.2 us, 71 MB = 3.9 TB/s.  A single small call takes 4 to 6 us.)
 //
 // G lanes share a token, the least power of two with 4 G >= E; a lane holds four scores: consecutive ones in one load if
 // E is a multiple of 4 (VEC), those of experts l, l + G, ... otherwise.  So a wave reads 64 / G neighbouring rows at a
@@ -324,34 +324,42 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_finish_kernel(const fl
 //   renorm 0: w_j = p[i_j]:                 ds_e = p_e (g_e - sum_l p_l g_l),  g_e = sum of d_topk_w[j] with i_j = e
 //   renorm 1: w = softmax over the chosen:  ds[i_j] = w_j (d_topk_w[j] - sum_l w_l d_topk_w[l])
 //   balance:  b_e = coef E k c_e / (sum c)^2, ds_e = p_e (b_e - sum_l p_l b_l)
-// ROUTING: d_topk_w is there.  ACC: d_scores is added to.
-template <int G, bool VEC, bool ROUTING, bool ACC>
+// Every lane finds out, for its experts, how often each was chosen (n_e) and g_e.
+// renorm 1 needs no more: with v_e = e^(s_e) / sum_l n_l e^(s_l),  ds_e = v_e (g_e - n_e sum_l v_l g_l) where n_e > 0.
+// Q: choices per lane, 0 without d_topk_w.  ACC: d_scores is added to.
+//
+// Up to one choice per lane, the choices' lanes write their numbers into a table of the wave's tokens and experts in LDS, from
+// which every lane reads who chose its experts; where a lane does not find its own number an expert was chosen twice, and
+// the wave goes through the choices one after the other, as it does for more choices.  (Measured, one after the other /
+// table, us: 65536 tokens, 128 experts, k = 8 24.2 / 18.2, renorm 1 28.2 / 22.0; 64, 6 13.9 / 11.7; 8 experts, two lanes
+// to a token, k = 2 4.4 / 4.6.)
+constexpr int GL_TABLE_FROM = 4;       // lanes of a token
+template <int G, bool VEC, int Q, bool ACC>
 __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float* __restrict__ scores,
                                                                     const int32_t* __restrict__ topk_idx,
                                                                     const float* __restrict__ d_topk_w,
                                                                     const int32_t* __restrict__ counts, float coef,
                                                                     const uint8_t* __restrict__ mask, int T, int E, int k,
                                                                     int renorm, int per_block, float* __restrict__ d_scores) {
+  __shared__ __align__(16) int table[Q == 1 && G >= GL_TABLE_FROM ? GL_THREADS / MOE_WAVE : 1][4 * MOE_WAVE];
   const int lane = lane_id(), l = lane % G;
   float b[4] = {};
   const bool with_p = counts || !renorm;             // the softmax over all experts has a part in it
   struct Row {
-    float s[4], old[4], d[4];
-    int e[4];
+    float s[4], old[4], d[Q > 0 ? Q : 1];
+    int e[Q > 0 ? Q : 1];
   };
   gl_rows<G, 2, Row>(
       T, per_block, mask, scores,
       [&](Row& r, int64_t t) {
         gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
         if constexpr (ACC) gl_load<G, VEC>(d_scores + t * E, E, l, 0.f, r.old);
-        if constexpr (ROUTING) {
-          // choices l, l + G, ... of the token are on lane l: k <= E <= 4 G
+        // choices l, l + G, ... of the token are on lane l: k <= E <= 4 G
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int64_t at = t * k + min(l + G * q, k - 1);
-            r.e[q] = topk_idx[at];
-            r.d[q] = d_topk_w[at];
-          }
+        for (int q = 0; q < Q; ++q) {
+          const int64_t at = t * k + min(l + G * q, k - 1);
+          r.e[q] = topk_idx[at];
+          r.d[q] = d_topk_w[at];
         }
       },
       [&] {
@@ -371,61 +379,79 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
         for (int j = 0; j < 4; ++j) b[j] *= c;
       },
       [&](Row& r, int64_t t, bool there, bool real) {
-        float p[4] = {}, d[4] = {}, chosen[4] = {};
-        if (with_p) gl_softmax<G>(r.s, p);
-        if constexpr (ROUTING) {
+        float p[4], d[4] = {}, g[4] = {}, times[4] = {};
+        bool distinct = false;
+        if constexpr (Q == 1 && G >= GL_TABLE_FROM) {
+          const bool chooses = l < k && static_cast<unsigned>(r.e[0]) < static_cast<unsigned>(E);
+          int* mine = &table[threadIdx.x / MOE_WAVE][lane / G * (4 * G)];
+          *reinterpret_cast<int4*>(mine + 4 * l) = make_int4(-1, -1, -1, -1);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          if (chooses) mine[r.e[0]] = lane;
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          distinct = !__any(chooses && mine[r.e[0]] != lane);
+          int from[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (l + G * q >= k || static_cast<unsigned>(r.e[q]) >= static_cast<unsigned>(E)) r.e[q] = -1, r.d[q] = 0.f;
-          if (renorm) {
-            float w[4], m = -INFINITY, sum = 0.f, dot = 0.f;
+          for (int j = 0; j < 4; ++j) from[j] = mine[gl_expert<G, VEC>(l, j)];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              w[q] = scores[t * E + max(r.e[q], 0)];
-              w[q] = r.e[q] >= 0 ? w[q] : -INFINITY;
-              m = fmaxf(m, w[q]);
-            }
-            m = gl_max<G>(m);
-            const bool some = m > -INFINITY;
-            const GlBase base(m);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              w[q] = __builtin_amdgcn_exp2f(base.exponent(w[q]));
-              sum += w[q];
-            }
-            sum = gl_sum<G>(sum);
-            const float inv = some ? 1.f / sum : 0.f;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              w[q] *= inv;
-              dot += w[q] * r.d[q];
-            }
-            dot = gl_sum<G>(dot);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) r.d[q] = w[q] * (r.d[q] - dot);
+          for (int j = 0; j < 4; ++j) {
+            const float v = __shfl(r.d[0], from[j]);
+            times[j] = from[j] >= 0 ? 1.f : 0.f;
+            g[j] = from[j] >= 0 ? v : 0.f;
           }
+        }
+        if (!distinct) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int j = 0; j < 4; ++j) g[j] = times[j] = 0.f;
+#pragma unroll
+          for (int q = 0; q < Q; ++q) {
             const int n = min(k - G * q, G);         // the same for all lanes
+            if (static_cast<unsigned>(r.e[q]) >= static_cast<unsigned>(E)) r.e[q] = -1;
             for (int i = 0; i < n; ++i) {
               const int e = __shfl(r.e[q], (lane & ~(G - 1)) + i);
               const float v = __shfl(r.d[q], (lane & ~(G - 1)) + i);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) chosen[j] += e == gl_expert<G, VEC>(l, j) ? v : 0.f;
+              for (int j = 0; j < 4; ++j) {
+                const bool same = e == gl_expert<G, VEC>(l, j);
+                g[j] += same ? v : 0.f;
+                times[j] += same ? 1.f : 0.f;
+              }
             }
           }
         }
-        if (with_p) {
-          float g[4];
+        if (Q > 0 && renorm) {
+          float v[4], sum = 0.f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) g[j] = renorm ? b[j] : b[j] + chosen[j];
+          for (int j = 0; j < 4; ++j) v[j] = times[j] > 0.f ? r.s[j] : -INFINITY;
+          const float m = gl_max<G>(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+          const GlBase base(m);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[j] = __builtin_amdgcn_exp2f(base.exponent(v[j]));
+            sum += times[j] * v[j];
+          }
+          sum = gl_sum<G>(sum);
+          const float inv = m > -INFINITY ? 1.f / sum : 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] *= inv;
+          const float dot = gl_sum<G>((v[0] * g[0] + v[1] * g[1]) + (v[2] * g[2] + v[3] * g[3]));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            d[j] = v[j] * (g[j] - times[j] * dot);
+            g[j] = 0.f;
+          }
+        }
+        if (with_p) {
+          gl_softmax<G>(r.s, p);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) g[j] += b[j];
           const float dot = gl_sum<G>((p[0] * g[0] + p[1] * g[1]) + (p[2] * g[2] + p[3] * g[3]));
 #pragma unroll
-          for (int j = 0; j < 4; ++j) d[j] = p[j] * (g[j] - dot);
+          for (int j = 0; j < 4; ++j) d[j] += p[j] * (g[j] - dot);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          d[j] = real ? d[j] + (renorm ? chosen[j] : 0.f) : 0.f;
+          d[j] = real ? d[j] : 0.f;
           if constexpr (ACC) d[j] += r.old[j];
         }
         if (there && (real || !ACC)) gl_store<G, VEC>(d_scores + t * E, E, l, d);
@@ -570,7 +596,7 @@ static GlPlan gl_plan(int T, int E, int threads, int U, int alone, int most_bloc
 static GlPlan gl_balance_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_SUM_THREADS, 2, 2, 256); }
 // One sum: as many blocks as the finishing block has threads.
 static GlPlan gl_distill_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 2, 2, GL_SUM_THREADS); }
-// (65536 tokens, 128 experts 24.7 us; with 2048 blocks 26.8.)
+// (2048 blocks instead of 1024: 65536 tokens, 128 experts 2 us more.)
 static GlPlan gl_route_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 2, 1, 1024); }
 
 // From this many tokens on the mask is counted by a launch of its own, not by every block.  (Measured, every block / a
@@ -632,8 +658,12 @@ extern "C" int moe_route_backward(const moe_shape_t* shape, const float* scores,
   gl_by_experts(E, [&](auto g, auto vec) {
     constexpr int G = decltype(g)::value;
     constexpr bool VEC = decltype(vec)::value;
-    const auto kernel = d_topk_w ? (accumulate ? route_backward_kernel<G, VEC, true, true> : route_backward_kernel<G, VEC, true, false>)
-                                 : (accumulate ? route_backward_kernel<G, VEC, false, true> : route_backward_kernel<G, VEC, false, false>);
+    const auto with = [&](auto q) {
+      return accumulate ? route_backward_kernel<G, VEC, decltype(q)::value, true> : route_backward_kernel<G, VEC, decltype(q)::value, false>;
+    };
+    const auto kernel = !d_topk_w ? with(std::integral_constant<int, 0>{})
+                        : k <= G  ? with(std::integral_constant<int, 1>{})
+                                  : with(std::integral_constant<int, 4>{});
     hipLaunchKernelGGL(kernel, dim3(plan.blocks), dim3(GL_THREADS), 0, st, scores, topk_idx, d_topk_w, counts, balance_coef, token_mask, T, E,
                        k, shape->renorm, plan.per_block, d_scores);
   });

@@ -201,6 +201,25 @@ def test_route_backward_of_odd_choices():
     check_route_backward(97, 16, 4, 0, None, scores, idx, None, np.arange(16, dtype=np.int64) * 100000000, 1e9, 0)
 
 
+@pytest.mark.parametrize("E,k", [(9, 3), (13, 4), (16, 4), (36, 9), (50, 16), (100, 7), (250, 64)])
+@pytest.mark.parametrize("renorm", [0, 1])
+def test_route_backward_of_a_few_odd_choices(E, k, renorm):
+    """Tokens that list an expert twice or three times among tokens that do not, and indices just behind the last expert."""
+    T = 700
+    rng, scores, idx = tables(T, E, k, 6)
+    dw = rng.standard_normal((T, k)).astype(np.float32)
+    idx[100, 1] = idx[100, 0]
+    idx[300:303, :3] = idx[300:303, :1]
+    idx[500] = idx[500, 0]
+    idx[200, 0], idx[201, k - 1], idx[202] = E, E + 1, E
+    check_route_backward(T, E, k, renorm, None, scores, idx, dw, go.balance_loss(scores, idx)[0], 0.5 * T, 0)
+    check_route_backward(T, E, k, renorm, mask_of("some", T, 5), scores, idx, dw, None, 0.0, 1)
+    dw[200, 0] = dw[201, k - 1] = dw[202, 0] = np.nan  # the weights of nobody
+    out = Guarded((T, E))
+    B.moe_route_backward(shape_of(T, E, k, renorm), dev(scores), dev(idx), dev(dw), None, 0.0, None, out.t)
+    assert np.isfinite(out.np()).all()
+
+
 def check_distill(T, E, mask, scores, target, coef, accumulate, with_grad=True):
     sh = shape_of(T, E, 1)
     ws, nb = workspace(sh)
