@@ -4,9 +4,9 @@
 //   moe_route_backward  the gradient of the routing weights and of coef * L
 //   moe_gate_distill    the mean over tokens of KL(softmax(target) || p), and its gradient
 // All three stream tables of T x E floats once: HBM-bound for large batches, launch-bound for small ones.  (Measured, in a
-// queue that is kept full, 65536 tokens: distill with a gradient, 128 experts 100 MB in 20.7 us = 4.9 TB/s and 27 with
-// the mask's count and the sum of the loss; balance and its gradient, 64 experts 21 us in three launches, 52 MB; route
-// backward, 128 experts, k = 8 18.2 us, 71 MB = 3.9 TB/s.  A single small call takes 4 to 6 us.)
+// queue that is kept full, 65536 tokens: distill with a gradient, 128 experts, 100 MB, 22.8 us, of it 4 for the sum of the
+// loss, and 26.8 with a mask; balance and its gradient, 64 experts, 52 MB, 18.4 us in three launches; route backward, 128
+// experts, k = 8, 71 MB, 15.8 us = 4.5 TB/s.  A single small call takes 4 to 6 us.)
 //
 // G lanes share a token, the least power of two with 4 G >= E; a lane holds four scores: consecutive ones in one load if
 // E is a multiple of 4 (VEC), those of experts l, l + G, ... otherwise.  So a wave reads 64 / G neighbouring rows at a
@@ -26,7 +26,8 @@ constexpr float GL_LOG2E = 1.44269504088896340736f;
 constexpr float GL_LN2 = 0.693147180559945309417f;
 
 // Sum and maximum over the G lanes of a token, on each of them: DPP steps inside a row of 16 lanes (xor 1, xor 2, then
-// the mirrors of 8 and of 16, as the lanes that they join hold equal values by then), exchanges beyond.
+// the mirrors of 8 and of 16, as the lanes that they join hold equal values by then), beyond it swaps, which leave the
+// even rows' (the lower half's) values in one register and the odd rows' (the upper half's) in the other.
 template <int CTRL> __device__ __forceinline__ float gl_dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
 }
@@ -35,8 +36,14 @@ template <int G, class Op> __device__ __forceinline__ float gl_reduce(float v, O
   if constexpr (G >= 4) v = op(v, gl_dpp<0x4E>(v));      // quad_perm [2,3,0,1]
   if constexpr (G >= 8) v = op(v, gl_dpp<0x141>(v));     // row_half_mirror
   if constexpr (G >= 16) v = op(v, gl_dpp<0x140>(v));    // row_mirror
-  if constexpr (G >= 32) v = op(v, __shfl_xor(v, 16));
-  if constexpr (G >= 64) v = op(v, __shfl_xor(v, 32));
+  if constexpr (G >= 32) {
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+  }
+  if constexpr (G >= 64) {
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+  }
   return v;
 }
 template <int G> __device__ __forceinline__ float gl_sum(float v) {
@@ -49,63 +56,77 @@ template <int G> __device__ __forceinline__ float gl_max(float v) {
 // The expert of value j of lane l of a token.
 template <int G, bool VEC> __device__ __forceinline__ int gl_expert(int l, int j) { return VEC ? 4 * l + j : l + G * j; }
 
+// Row `row` of a block's rows of a table of `width` columns of 4 bytes.  (The block's rows have less than 2^32 bytes, being
+// 1/256 of a table at most, and number less than 2^24: the table's address stays in scalar registers.)
+template <class V> __device__ __forceinline__ V* gl_row(V* rows, int row, int width, int column) {
+  const uint32_t at = __umul24(row, 4 * width) + 4 * column;
+  if constexpr (std::is_const<V>::value)
+    return reinterpret_cast<V*>(reinterpret_cast<const char*>(rows) + at);
+  else
+    return reinterpret_cast<V*>(reinterpret_cast<char*>(rows) + at);
+}
+
 // A lane's four values of a row of a table, `fill` past the last expert.  (No load is behind a branch: lanes past the end
 // read the last values again.  The compiler counts on no load that a branch may skip, and would wait for all of them.)
 template <int G, bool VEC>
-__device__ __forceinline__ void gl_load(const float* __restrict__ row, int E, int l, float fill, float (&v)[4]) {
+__device__ __forceinline__ void gl_load(const float* __restrict__ rows, int row, int E, int l, float fill, float (&v)[4]) {
   if constexpr (VEC) {
-    const float4 q = *reinterpret_cast<const float4*>(row + min(4 * l, E - 4));
+    const float4 q = *reinterpret_cast<const float4*>(gl_row(rows, row, E, min(4 * l, E - 4)));
     const bool there = 4 * l < E;
     v[0] = there ? q.x : fill, v[1] = there ? q.y : fill, v[2] = there ? q.z : fill, v[3] = there ? q.w : fill;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int e = l + G * j;
-      v[j] = row[min(e, E - 1)];
+      v[j] = *gl_row(rows, row, E, min(e, E - 1));
       v[j] = e < E ? v[j] : fill;
     }
   }
 }
 
-template <int G, bool VEC> __device__ __forceinline__ void gl_store(float* __restrict__ row, int E, int l, const float (&v)[4]) {
+template <int G, bool VEC> __device__ __forceinline__ void gl_store(float* __restrict__ rows, int row, int E, int l, const float (&v)[4]) {
   if constexpr (VEC) {
-    if (4 * l < E) *reinterpret_cast<float4*>(row + 4 * l) = make_float4(v[0], v[1], v[2], v[3]);
+    if (4 * l < E) *reinterpret_cast<float4*>(gl_row(rows, row, E, 4 * l)) = make_float4(v[0], v[1], v[2], v[3]);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int e = l + G * j;
-      if (e < E) row[e] = v[j];
+      if (e < E) *gl_row(rows, row, E, e) = v[j];
     }
   }
 }
 
-// c (s - m) of a row with the maximum m.  Where c m could pass the largest number (scores of the type's lowest value) m is
-// subtracted first; -inf: every s is, and the results are not used.
-struct GlBase {
-  float shift, scaled;
-  __device__ __forceinline__ explicit GlBase(float m) {
-    const bool far = fabsf(m) > 1e30f;
-    shift = far && m > -INFINITY ? m : 0.f;
-    scaled = far ? 0.f : GL_LOG2E * m;
+// The exponents c (s - m) of a row with the maximum m.  Where c m could pass the largest number (scores of the type's lowest
+// value) m is subtracted first; m = -inf: every s is, and so are the exponents.
+__device__ __forceinline__ void gl_exponents(const float (&s)[4], float m, float (&t)[4]) {
+  const bool far = fabsf(m) > 1e30f;
+  float scaled = GL_LOG2E * m;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[j] = s[j];
+  if (__any(far)) {                                  // rarely
+    const float shift = far && m > -INFINITY ? m : 0.f;
+    scaled = far ? 0.f : scaled;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t[j] -= shift;
   }
-  __device__ __forceinline__ float exponent(float s) const { return fmaf(GL_LOG2E, s - shift, -scaled); }
-};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[j] = fmaf(GL_LOG2E, t[j], -scaled);
+}
+
+// 1 / v for a sum of powers, one of which is 1: v_rcp_f32, off by 2^-23 at most.
+__device__ __forceinline__ float gl_inverse(float v) { return __builtin_amdgcn_rcpf(v); }
 
 // p = softmax of a row, zeros where every score is -inf.  log2p: its logarithms (of base 2).  Returns whether anything
 // is left of the row.
 template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4], float (&p)[4], float (*log2p)[4] = nullptr) {
   const float m = gl_max<G>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
   const bool some = m > -INFINITY;
-  const GlBase base(m);
-  float t[4], sum = 0.f;
+  float t[4];
+  gl_exponents(s, m, t);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    t[j] = base.exponent(s[j]);
-    p[j] = __builtin_amdgcn_exp2f(t[j]);
-    sum += p[j];
-  }
-  sum = gl_sum<G>(sum);
-  const float inv = some ? 1.f / sum : 0.f;
+  for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(t[j]);
+  const float sum = gl_sum<G>((p[0] + p[1]) + (p[2] + p[3]));
+  const float inv = some ? gl_inverse(sum) : 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) p[j] *= inv;
   if (log2p) {
@@ -128,42 +149,42 @@ template <class V> __device__ __forceinline__ V gl_block_sum(V v, V* lds) {
   return v;
 }
 
-// The rows of a block (which has one or more), in turns of its waves, U batches of 64 / G rows at a time: load(data, row) of
-// all of them, then use(data, row, whether there is such a row, whether it counts) of each.  The loads of a turn are on
-// their way during the turn before, those of the first during `first`; past the end the last row is read again.
-// `table`: T bytes or more, read where there is no mask.
-template <int G, int U, class Data, class Load, class First, class Use>
-__device__ __forceinline__ void gl_rows(int T, int per_block, const uint8_t* __restrict__ mask, const void* table, Load load, First first,
-                                        Use use) {
+// A block's rows: the first one, and their number.
+struct GlRows {
+  int64_t begin;
+  int n;
+  __device__ __forceinline__ GlRows(int T, int per_block)
+      : begin(static_cast<int64_t>(blockIdx.x) * per_block), n(static_cast<int>(min(static_cast<int64_t>(per_block), T - begin))) {}
+};
+
+// The n > 0 rows of a block, in turns of its waves, 64 / G rows at a time: load(data, row), then use(data, row, whether there
+// is such a row, whether it counts); rows are counted from the block's first, as are the bytes of `mask`.  The loads of a
+// turn are on their way during the turn before, those of the first during `first`; past the end the last row is read again.
+// `table`: n bytes or more, read where there is no mask.  (Two batches of rows to a turn: route backward of 65536 tokens, 64
+// experts 12.7 us instead of 12.0, of 4096 tokens, 128 experts 4.9 instead of 4.5.)
+template <int G, class Data, class Load, class First, class Use>
+__device__ __forceinline__ void gl_rows(int n, const uint8_t* __restrict__ mask, const void* table, Load load, First first, Use use) {
   constexpr int ROWS = MOE_WAVE / G;
-  const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
-  const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
   struct Turn {
-    Data data[U];
-    uint8_t mask[U];
+    Data data;
+    uint8_t mask;
   };
   const uint8_t* some_bytes = mask ? mask : static_cast<const uint8_t*>(table);
-  auto start = [&](Turn& n, int64_t t0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t row = min(t0 + u * ROWS + lane_id() / G, end - 1);
-      n.mask[u] = some_bytes[row];
-      load(n.data[u], row);
-    }
+  auto start = [&](Turn& next, int t0) {
+    const int row = min(t0 + lane_id() / G, n - 1);
+    next.mask = some_bytes[static_cast<uint32_t>(row)];
+    load(next.data, row);
   };
-  const int64_t step = blockDim.x / MOE_WAVE * (ROWS * U);
-  int64_t t0 = begin + threadIdx.x / MOE_WAVE * (ROWS * U);
+  const int step = blockDim.x / MOE_WAVE * ROWS;
+  int t0 = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE) * ROWS;
   Turn now;
   start(now, t0);
   first();
-  while (t0 < end) {
+  while (t0 < n) {
     Turn next;
     start(next, t0 + step);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * ROWS + lane_id() / G;
-      use(now.data[u], min(t, end - 1), t < end, t < end && (!mask || now.mask[u]));
-    }
+    const int t = t0 + lane_id() / G;
+    use(now.data, t, t < n, t < n && (!mask || now.mask));
     now = next;
     t0 += step;
   }
@@ -210,17 +231,20 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_kernel(const float* __
   struct Row {
     float s[4];
   };
-  gl_rows<G, 2, Row>(
-      T, per_block, mask, scores, [&](Row& r, int64_t t) { gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s); },
+  const GlRows rows(T, per_block);
+  scores += rows.begin * E;
+  topk_idx += rows.begin * k;
+  if (mask) mask += rows.begin;
+  gl_rows<G, Row>(
+      rows.n, mask, scores, [&](Row& r, int t) { gl_load<G, VEC>(scores, t, E, l, -INFINITY, r.s); },
       [&] {
-        const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_block;
-        const int64_t end = min(begin + per_block, static_cast<int64_t>(T));
-        for (int64_t a = begin * k + threadIdx.x; a < end * k; a += GL_SUM_THREADS) {
+        const uint32_t choices = static_cast<uint32_t>(rows.n) * k;      // T k < 2^31
+        for (uint32_t a = threadIdx.x; a < choices; a += GL_SUM_THREADS) {
           const int e = topk_idx[a];
           if ((!mask || mask[a / k]) && static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(&cnt[e], 1);
         }
       },
-      [&](Row& r, int64_t, bool, bool real) {
+      [&](Row& r, int, bool, bool real) {
         float p[4];
         gl_softmax<G>(r.s, p);
 #pragma unroll
@@ -349,17 +373,22 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
     float s[4], old[4], d[Q > 0 ? Q : 1];
     int e[Q > 0 ? Q : 1];
   };
-  gl_rows<G, 2, Row>(
-      T, per_block, mask, scores,
-      [&](Row& r, int64_t t) {
-        gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
-        if constexpr (ACC) gl_load<G, VEC>(d_scores + t * E, E, l, 0.f, r.old);
+  const GlRows rows(T, per_block);
+  scores += rows.begin * E;
+  d_scores += rows.begin * E;
+  if (Q > 0) topk_idx += rows.begin * k, d_topk_w += rows.begin * k;
+  if (mask) mask += rows.begin;
+  gl_rows<G, Row>(
+      rows.n, mask, scores,
+      [&](Row& r, int t) {
+        gl_load<G, VEC>(scores, t, E, l, -INFINITY, r.s);
+        if constexpr (ACC) gl_load<G, VEC>(d_scores, t, E, l, 0.f, r.old);
         // choices l, l + G, ... of the token are on lane l: k <= E <= 4 G
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-          const int64_t at = t * k + min(l + G * q, k - 1);
-          r.e[q] = topk_idx[at];
-          r.d[q] = d_topk_w[at];
+          const int choice = min(l + G * q, k - 1);
+          r.e[q] = *gl_row(topk_idx, t, k, choice);
+          r.d[q] = *gl_row(d_topk_w, t, k, choice);
         }
       },
       [&] {
@@ -378,7 +407,7 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
 #pragma unroll
         for (int j = 0; j < 4; ++j) b[j] *= c;
       },
-      [&](Row& r, int64_t t, bool there, bool real) {
+      [&](Row& r, int t, bool there, bool real) {
         float p[4], d[4] = {}, g[4] = {}, times[4] = {};
         bool distinct = false;
         if constexpr (Q == 1 && G >= GL_TABLE_FROM) {
@@ -420,18 +449,18 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
           }
         }
         if (Q > 0 && renorm) {
-          float v[4], sum = 0.f;
+          float v[4], t[4], sum = 0.f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] = times[j] > 0.f ? r.s[j] : -INFINITY;
           const float m = gl_max<G>(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
-          const GlBase base(m);
+          gl_exponents(v, m, t);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            v[j] = __builtin_amdgcn_exp2f(base.exponent(v[j]));
+            v[j] = __builtin_amdgcn_exp2f(t[j]);
             sum += times[j] * v[j];
           }
           sum = gl_sum<G>(sum);
-          const float inv = m > -INFINITY ? 1.f / sum : 0.f;
+          const float inv = m > -INFINITY ? gl_inverse(sum) : 0.f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] *= inv;
           const float dot = gl_sum<G>((v[0] * g[0] + v[1] * g[1]) + (v[2] * g[2] + v[3] * g[3]));
@@ -454,7 +483,7 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
           d[j] = real ? d[j] : 0.f;
           if constexpr (ACC) d[j] += r.old[j];
         }
-        if (there && (real || !ACC)) gl_store<G, VEC>(d_scores + t * E, E, l, d);
+        if (there && (real || !ACC)) gl_store<G, VEC>(d_scores, t, E, l, d);
       });
 }
 
@@ -509,18 +538,22 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
   struct Row {
     float s[4], u[4], old[4];
   };
-  gl_rows<G, 2, Row>(
-      T, per_block, mask, scores,
-      [&](Row& r, int64_t t) {
-        gl_load<G, VEC>(scores + t * E, E, l, -INFINITY, r.s);
-        gl_load<G, VEC>(target + t * E, E, l, -INFINITY, r.u);
-        if constexpr (ACC) gl_load<G, VEC>(d_scores + t * E, E, l, 0.f, r.old);
+  const GlRows rows(T, per_block);
+  scores += rows.begin * E;
+  target += rows.begin * E;
+  if (d_scores) d_scores += rows.begin * E;
+  gl_rows<G, Row>(
+      rows.n, mask ? mask + rows.begin : nullptr, scores,
+      [&](Row& r, int t) {
+        gl_load<G, VEC>(scores, t, E, l, -INFINITY, r.s);
+        gl_load<G, VEC>(target, t, E, l, -INFINITY, r.u);
+        if constexpr (ACC) gl_load<G, VEC>(d_scores, t, E, l, 0.f, r.old);
       },
       [&] {
         n = gl_tokens(mask, part_n, T, lds_n);
         scale = n > 0.0 ? static_cast<float>(coef / n) : 0.f;
       },
-      [&](Row& r, int64_t t, bool there, bool real) {
+      [&](Row& r, int t, bool there, bool real) {
         float p[4], q[4], lp[4], lq[4], d[4];
         const bool left_p = gl_softmax<G>(r.s, p, &lp), left_q = gl_softmax<G>(r.u, q, &lq);
         const bool counts = real && left_p && left_q;
@@ -532,7 +565,7 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
           if constexpr (ACC) d[j] += r.old[j];
         }
         sum += counts ? row : 0.f;
-        if (d_scores && there && (real || !ACC)) gl_store<G, VEC>(d_scores + t * E, E, l, d);
+        if (d_scores && there && (real || !ACC)) gl_store<G, VEC>(d_scores, t, E, l, d);
       });
   sum = gl_block_sum(sum * GL_LN2, lds);
   if (threadIdx.x != 0) return;
@@ -577,27 +610,27 @@ static int gl_lanes(int E) {
   return g;
 }
 
-// Blocks of a call and the rows of each: a pass of the block's waves (U batches of rows each), or as many as the limit on
-// blocks asks for; a batch of up to `alone` passes is one block, which needs no launch to add up sums.  (Measured, one
-// block / two launches, us: balance 64 experts, 200 tokens 8.5 / 10.4, 500 11.5 / 10.7; 8 experts, 2000 tokens 9.0 / 12.1;
-// distill 8 experts, 500 tokens 4.0 / 5.6, 3000 11.8 / 5.8; 64 experts, 120 tokens 6.2 / 5.8.)
+// Blocks of a call and the rows of each: a turn of the block's waves, or as many as the limit on
+// blocks asks for; a batch of up to `alone` turns is one block, which needs no launch to add up sums.  (Measured, one
+// block / two launches, us: balance 64 experts, 200 tokens 7.4 / 9.3, 500 9.5 / 9.4; 8 experts, 1500 tokens 7.5 / 11.2;
+// distill 8 experts, 500 tokens 4.0 / 5.2, 64 experts, 60 tokens 4.1 / 5.3, 120 5.7 / 5.4.)
 struct GlPlan {
   int blocks, per_block;
 };
-static GlPlan gl_plan(int T, int E, int threads, int U, int alone, int most_blocks) {
-  const int64_t pass = static_cast<int64_t>(threads) / gl_lanes(E) * U;
+static GlPlan gl_plan(int T, int E, int threads, int alone, int most_blocks) {
+  const int64_t pass = threads / gl_lanes(E);
   int64_t per = (static_cast<int64_t>(T) + most_blocks - 1) / most_blocks;
   per = (per + pass - 1) / pass * pass;
   if (T <= alone * pass) per = T;
   return {T > 0 ? static_cast<int>((T + per - 1) / per) : 0, static_cast<int>(per)};
 }
 // Sums for every expert: one block adds up the blocks' rows, so there are 256 blocks at most (65536 tokens, 64 experts
-// 21.0 us; with 512 blocks 24.4).
-static GlPlan gl_balance_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_SUM_THREADS, 2, 2, 256); }
-// One sum: as many blocks as the finishing block has threads.
-static GlPlan gl_distill_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 2, 2, GL_SUM_THREADS); }
-// (2048 blocks instead of 1024: 65536 tokens, 128 experts 2 us more.)
-static GlPlan gl_route_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 2, 1, 1024); }
+// 18.4 us; with 512 blocks 21.0).
+static GlPlan gl_balance_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_SUM_THREADS, 4, 256); }
+// One sum: as many blocks as the finishing block has threads (65536 tokens, 128 experts 22.8 us; with half as many 25.9).
+static GlPlan gl_distill_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 4, GL_SUM_THREADS); }
+// (512 / 1024 / 2048 blocks: 65536 tokens, 128 experts 17.9 / 15.8 / 16.0 us, 64 experts 12.8 / 12.0 / 12.5.)
+static GlPlan gl_route_plan(const moe_shape_t* s) { return gl_plan(s->T, s->E, GL_THREADS, 1, 1024); }
 
 // From this many tokens on the mask is counted by a launch of its own, not by every block.  (Measured, every block / a
 // launch, us: E = 64, 4000 tokens 7.7 / 9.7, 16384 9.4 / 10.3, 30000 14.5 / 14.7; E = 128, 65536 tokens 31.1 / 27.2.)
