@@ -347,7 +347,8 @@ __global__ __launch_bounds__(GL_SUM_THREADS) void balance_finish_kernel(const fl
 // ds = gradient of sum_j d_topk_w[j] w_j (w: the routing weights of moe_route) + gradient of coef * L.
 //   renorm 0: w_j = p[i_j]:                 ds_e = p_e (g_e - sum_l p_l g_l),  g_e = sum of d_topk_w[j] with i_j = e
 //   renorm 1: w = softmax over the chosen:  ds[i_j] = w_j (d_topk_w[j] - sum_l w_l d_topk_w[l])
-//   balance:  b_e = coef E k c_e / (sum c)^2, ds_e = p_e (b_e - sum_l p_l b_l)
+//   balance:  b_e = coef E k c_e / (sum c)^2, ds_e = p_e (b_e - sum_l p_l b_l);  as the p_l add up to 1 a constant may be
+//             taken off the b_e, their mean: what is left of even loads is then not the rounding of large numbers
 // Every lane finds out, for its experts, how often each was chosen (n_e) and g_e.
 // renorm 1 needs no more: with v_e = e^(s_e) / sum_l n_l e^(s_l),  ds_e = v_e (g_e - n_e sum_l v_l g_l) where n_e > 0.
 // Q: choices per lane, 0 without d_topk_w.  ACC: d_scores is added to.
@@ -396,16 +397,13 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
         int64_t total = 0;
         for (int e = lane; e < E; e += MOE_WAVE) total += counts[e];
 #pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
+        const double n = static_cast<double>(total), c = total > 0 ? static_cast<double>(coef) * k / (n * n) : 0.0;
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int e = gl_expert<G, VEC>(l, j);
-          if (e < E) b[j] = static_cast<float>(counts[e]);
+          if (e < E) b[j] = static_cast<float>(c * static_cast<double>(static_cast<int64_t>(counts[e]) * E - total));
         }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off);
-        const double n = static_cast<double>(total);
-        const float c = total > 0 ? static_cast<float>(static_cast<double>(coef) * E * k / (n * n)) : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] *= c;
       },
       [&](Row& r, int t, bool there, bool real) {
         float p[4], d[4] = {}, g[4] = {}, times[4] = {};

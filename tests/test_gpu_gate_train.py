@@ -201,6 +201,14 @@ def test_route_backward_of_odd_choices():
     check_route_backward(97, 16, 4, 0, None, scores, idx, None, np.arange(16, dtype=np.int64) * 100000000, 1e9, 0)
 
 
+@pytest.mark.parametrize("E", [1, 8, 60, 256])
+def test_even_loads_have_no_balance_gradient(E):
+    _, scores, _ = tables(300, E, 1, 7, spread=3.0)
+    out = Guarded((300, E))
+    B.moe_route_backward(shape_of(300, E, 1), dev(scores), None, None, torch.full((E,), 12345, dtype=torch.int32, device="cuda"), 1e4, None, out.t)
+    assert not out.np().any()
+
+
 @pytest.mark.parametrize("E,k", [(9, 3), (13, 4), (16, 4), (36, 9), (50, 16), (100, 7), (250, 64)])
 @pytest.mark.parametrize("renorm", [0, 1])
 def test_route_backward_of_a_few_odd_choices(E, k, renorm):
