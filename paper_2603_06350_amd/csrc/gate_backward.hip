@@ -71,6 +71,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t gb_rows(const void* first, int
   const uint32_t n = __builtin_amdgcn_readfirstlane(max(rows, 0));
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(first), 0, static_cast<int>(n * pitch), 0x00020000);
 }
+// The same number, but nothing that is computed from it is kept from one step to the next: sixteen offsets of rows would
+// take as many registers, where an addition for each is cheap.
+__device__ __forceinline__ uint32_t gb_anew(uint32_t v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
 __device__ __forceinline__ float gb_load_f32(__amdgpu_buffer_rsrc_t rows, uint32_t at) {
   return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rows, static_cast<int>(at), 0, 0));
 }
@@ -298,12 +304,15 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
 // in LDS in the order in which the lanes want them: thread 64 w + i of a step cuts 8 tokens (8 (w % 4) of half w / 4) of
 // expert i.
 //
-// A step's loads are on their way while the one before is multiplied.  For 65536 tokens, d = 2048, E = 64 the loads alone
-// take 45 us, the rest alone 43, both together 62 (the clock falls to about 1.95 GHz under the matrix instructions).  Loads
-// four steps ahead with one wave per SIMD, loads between the products, and two blocks of four waves were not faster.
+// A step's loads are on their way while the one before is multiplied.  Measured, us: 16384 tokens, d = 4096, E = 128 50.6
+// (its matrix instructions alone 26, without products 43), 65536 tokens 182; d = 2048, E = 64, 65536 tokens 63 (without
+// products 60).  Where the waves met between two steps, with all of them splitting and transposing at the same time, it
+// was 55.4, 202, 63.  Loads four steps ahead with one wave per SIMD, loads between the products, and two blocks of four
+// waves were not faster.
 constexpr int GWW_PIECES = 4 * MOE_WAVE * 16;         // bytes of a piece of 32 tokens, 64 experts
 constexpr int GWW_STEP = 2 * 3 * GWW_PIECES;
-constexpr int GWW_LDS = 2 * GWW_STEP > GW_WAVES * 8 * MOE_WAVE * 16 ? 2 * GWW_STEP : GW_WAVES * 8 * MOE_WAVE * 16;
+constexpr int GWW_LDS = 3 * GWW_STEP;                 // (the waves' sums need 64 KiB of it)
+static_assert(GWW_LDS >= GW_WAVES * 8 * MOE_WAVE * 16, "sums of the waves");
 
 template <bool BF16, int V>
 __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned char* lds, float* red_b) {
@@ -326,27 +335,29 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
   float ds[8], bias = 0.f;
   GbRow<BF16, V> x[8];
   uint32_t mask;
-  auto load = [&](uint32_t t0) {
-    const int left = static_cast<int>(end - t0) - 32 * half;
+  auto left_of = [&](uint32_t t0) { return min(static_cast<int>(end - t0) - 32 * half, 32); };
+  auto load_x = [&](uint32_t t0) {
+    const auto rows = gb_rows(a.x + (static_cast<int64_t>(t0) + 32 * half) * pitch, with_w ? left_of(t0) : 0, pitch);
+    const uint32_t p = gb_anew(pitch);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j].load(rows, at_x + j * p);
+  };
+  auto load_s = [&](uint32_t t0) {
     const int64_t t = static_cast<int64_t>(t0) + 32 * half;
+    const auto rows = gb_rows(reinterpret_cast<const char*>(a.d_scores) + t * pitch_s, left_of(t0), pitch_s);
+    const uint32_t p = gb_anew(pitch_s);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      ds[j] = gb_load_f32(gb_rows(reinterpret_cast<const char*>(a.d_scores) + (t + j) * pitch_s, min(left, 32) - j, pitch_s), at_s);
-    mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t, a.mask ? min(left, 32) : 0, 1), lane & 31, 0, 0);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j].load(gb_rows(a.x + (t + j) * pitch, with_w ? min(left, 32) - j : 0, pitch), at_x);
+    for (int j = 0; j < 8; ++j) ds[j] = gb_load_f32(rows, at_s + j * p);
+    mask = __builtin_amdgcn_raw_buffer_load_b8(gb_rows(a.mask + t, a.mask ? left_of(t0) : 0, 1), lane & 31, 0, 0);
   };
-  // bit i: token t0 + 32 half + i counts
-  auto reals = [&](uint32_t t0) {
-    const int left = static_cast<int>(end - t0) - 32 * half;
-    return static_cast<uint32_t>(__ballot((lane & 31) < left && (!a.mask || mask)));
-  };
-  auto some_padded = [&](uint32_t t0) { return a.mask || static_cast<int>(end - t0) < 64; };
+  // Pieces of a step's gradients, of which bit i of the result says whether token t0 + 32 half + i counts.
   auto put = [&](uint32_t t0, unsigned char* to) {
-    if (some_padded(t0)) {
-      const uint32_t real = reals(t0) >> (8 * (wave & 3));
+    uint32_t real = 0xFFFFFFFFu;
+    if (a.mask || static_cast<int>(end - t0) < 64) {
+      real = static_cast<uint32_t>(__ballot((lane & 31) < left_of(t0) && (!a.mask || mask)));
+      const uint32_t mine = real >> (8 * (wave & 3));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ds[j] = real >> j & 1 ? ds[j] : 0.f;
+      for (int j = 0; j < 8; ++j) ds[j] = mine >> j & 1 ? ds[j] : 0.f;
     }
     if (with_bias) {
 #pragma unroll
@@ -356,6 +367,7 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
     gb_split8(ds, p);
 #pragma unroll
     for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + at_piece + q * GWW_PIECES) = p[q];
+    return real;
   };
 
   gb_f32x4 acc[MT][V];
@@ -363,36 +375,43 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[m][i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
-  // A step's operands go over to the registers that the products read, and the next step's are requested into the ones
-  // that are free then; behind the last step nothing is read.
-  load(begin);
-  put(begin, lds);
+  // x of a step goes over to the registers that the products read, and the next step's is requested into the ones that are
+  // free then.  The next step's gradients, which are a step ahead of x, are cut into pieces halfway through the products:
+  // the waves meet there, and need not start the next step together.  A third place for pieces in LDS is for the waves
+  // that are behind by half a step.  Behind the last step nothing is read.
+  load_s(begin);
+  load_x(begin);
+  uint32_t real = put(begin, lds);
+  load_s(begin + 64);
   __syncthreads();
   uint32_t at_lds = 0;
-  for (uint32_t t0 = begin; t0 < end; at_lds = GWW_STEP - at_lds) {
-    if (some_padded(t0)) {
-      const uint32_t real = reals(t0) >> (8 * g);
+  for (uint32_t t0 = begin; t0 < end; t0 += 64) {
+    if (real != 0xFFFFFFFFu) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j].keep(real >> j & 1);
+      for (int j = 0; j < 8; ++j) x[j].keep(real >> (8 * g) >> j & 1);
     }
     GbFrag<BF16, V> b;
     gb_transpose<BF16, V>(x, b);
     __builtin_amdgcn_sched_barrier(0);
-    t0 += 64;
-    load(t0);
+    load_x(t0 + 64);
     __builtin_amdgcn_sched_barrier(0);
+    const uint32_t next = at_lds == 2 * GWW_STEP ? 0 : at_lds + GWW_STEP;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
+      if (m == MT / 2) {
+        real = put(t0 + 64, lds + next);
+        load_s(t0 + 128);
+        __syncthreads();
+      }
       uint4 p[3];
 #pragma unroll
       for (int q = 0; q < 3; ++q)
         p[q] = *reinterpret_cast<const uint4*>(lds + at_lds + (half * 3 + q) * GWW_PIECES + (m * MOE_WAVE + lane) * 16);
       gb_products<BF16, false, V>(p[0], p[1], p[2], b, acc[m]);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    put(t0, lds + (GWW_STEP - at_lds));
-    __syncthreads();
+    at_lds = next;
   }
+  __syncthreads();
 
   // The halves' sums meet in LDS: the first half's waves finish the experts 0..31, the second's 32..63.
   const int64_t n = static_cast<int64_t>(E) * d;
