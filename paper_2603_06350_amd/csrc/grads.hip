@@ -1,8 +1,8 @@
 // moe_grad_norm, moe_clip_grads: the Euclidean norm of a list of tensors taken together, and the tensors scaled to a
 // largest norm:  norm = sqrt(sum over all elements of g^2),  out = g * min(1, max_norm / norm).
 // HBM-bound: every element is read once for the norm, and once more with a write for the scaling.  (Measured: 60 tensors
-// of 5 to 14336 x 4096 elements, 844 MB of fp32 and bf16, 459 us, of it the norm 143 = 5.9 TB/s and the scaling 310 =
-// 5.4 TB/s read and written; 32 tensors of 512 KiB 11.6 us.)
+// of 5 to 14336 x 4096 elements, 844 MB of fp32 and bf16, 447 us, of it the norm 143 = 5.9 TB/s and the scaling 300 =
+// 5.6 TB/s read and written; 32 tensors of 512 KiB 11.6 us.)
 //
 // The list travels in the kernels' arguments, so no table has to reach the device first and a captured graph holds its
 // own copy.  Every block takes one piece of one tensor.  Squares and their sums are 64-bit (an fp32 square overflows
@@ -54,8 +54,9 @@ __device__ __forceinline__ GradPiece grad_piece(const GradTable& tab, int count,
 }
 
 // The elements [begin, end) of a tensor: those in whole, aligned 16-byte chunks by `chunk`(pointer to it, its first
-// element's number), the others, at most 7 at either end, by `one`(number).
-template <bool BF16, class Chunk, class One>
+// element's number), the others, at most 7 at either end, by `one`(number).  LAST: nothing is read again.  (The scaling's
+// loads marked so, us: 844 MB 458 -> 447, 512 MiB of bf16 280 -> 270, 40 tensors of up to 2000000 21.0 -> 20.4.)
+template <bool BF16, bool LAST, class Chunk, class One>
 __device__ __forceinline__ void grad_for_each(const GradPiece& g, Chunk chunk, One one) {
   constexpr int PER = BF16 ? 8 : 4, UNROLL = 4;
   const int64_t skip = -static_cast<int64_t>(reinterpret_cast<uintptr_t>(g.data) / (16 / PER)) & (PER - 1);   // elements before an aligned one
@@ -70,7 +71,7 @@ __device__ __forceinline__ void grad_for_each(const GradPiece& g, Chunk chunk, O
   for (; i + (UNROLL - 1) * GR_THREADS < n; i += UNROLL * GR_THREADS) {
     uint4 v[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) v[u] = p[i + u * GR_THREADS];
+    for (int u = 0; u < UNROLL; ++u) v[u] = LAST ? nt_load(p + i + u * GR_THREADS) : p[i + u * GR_THREADS];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) chunk(v[u], first + (i + u * GR_THREADS) * PER);
   }
@@ -95,7 +96,7 @@ template <bool BF16> __device__ __forceinline__ double grad_squares(const GradPi
     const double d = f;
     s[k & 3] = fma(d, d, s[k & 3]);
   };
-  grad_for_each<BF16>(
+  grad_for_each<BF16, false>(
       g,
       [&](uint4 v, int64_t) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -144,7 +145,7 @@ template <bool BF16> __device__ __forceinline__ void grad_scale(const GradPiece&
     for (int64_t i = g.begin + threadIdx.x; i < g.end; i += GR_THREADS) one(i);
     return;
   }
-  grad_for_each<BF16>(
+  grad_for_each<BF16, true>(
       g,
       [&](uint4 v, int64_t i) {
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
