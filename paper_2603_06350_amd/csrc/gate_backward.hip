@@ -5,9 +5,10 @@
 // HBM; beyond, the weights' gradient has as much to do in the matrix instructions and the splitting into pieces as in its
 // loads, and neither hides the other entirely.
 //
-// Measured (bf16 layers, a copy on this card reads and writes 4.6 to 5.4 TB/s, us): d = 4096, E = 8, 65536 tokens both
-// gradients 234 (4.6 TB/s); d = 2048, E = 64, 65536 tokens weights 62 to 75 + sums 6.5, hidden states 48 to 52 (5.4 TB/s
-// written); d = 4096, E = 128, 16384 tokens weights only 58 + sums 9.7.
+// Measured (bf16 layers; a copy on this card reads and writes 4.6 to 5.4 TB/s): both gradients of 65536 tokens, d = 4096, E = 8
+// 217 us = 5.0 TB/s; 65536 tokens, d = 2048, E = 64 111 us = 5.0 TB/s, of it the weights' 56
+// with 6.5 for the sums of the parts and the hidden states' 47 = 5.7 TB/s written; weights alone of 16384 tokens, d = 4096,
+// E = 128 50 us and 9.6.
 //
 // Both run on v_mfma_f32_16x16x32_bf16 with fp32 accumulators, operands straight from global memory into registers:
 //   - a lane that holds V consecutive columns of 8 consecutive rows of a matrix (one load per row) turns them, with
@@ -311,11 +312,11 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
 // in LDS in the order in which the lanes want them: thread 64 w + i of a step cuts 8 tokens (8 (w % 4) of half w / 4) of
 // expert i.
 //
-// A step's loads are on their way while the one before is multiplied.  Measured, us: 16384 tokens, d = 4096, E = 128 50.6
-// (its matrix instructions alone 26, without products 43), 65536 tokens 182; d = 2048, E = 64, 65536 tokens 63 (without
-// products 60).  Where the waves met between two steps, with all of them splitting and transposing at the same time, it
-// was 55.4, 202, 63.  Loads four steps ahead with one wave per SIMD, loads between the products, and two blocks of four
-// waves were not faster.
+// A step's loads are on their way while the one before is multiplied.  Measured, us: 16384 tokens, d = 4096, E = 128 50 (its
+// matrix instructions alone 26, without products 43), 65536 tokens 171; d = 2048, E = 64, 65536 tokens 58.  Where the waves
+// met between two steps, all of them splitting and transposing at the same time, it took 10 % longer with 128 experts.
+// Loads one, two and four steps further ahead (spills, or one wave per SIMD), loads between the products, the 32x32x16
+// instruction (1.9 PFLOP/s in a loop of its own, the 16x16x32 2.0 to 2.2), and two blocks of four waves were not faster.
 constexpr int GWW_PIECES = 4 * MOE_WAVE * 16;         // bytes of a piece of 32 tokens, 64 experts
 constexpr int GWW_STEP = 2 * 3 * GWW_PIECES;
 constexpr int GWW_LDS = 3 * GWW_STEP;                 // (the waves' sums need 64 KiB of it)
@@ -708,8 +709,8 @@ __global__ __launch_bounds__(GW_THREADS, MT == 1 && !ACC ? 4 : 2) void gate_narr
 //
 // More than 32 experts: blocks of 32 read x once for every 32, blocks of 64 are four times as wide and leave that many more
 // parts to be added up.  So the former take what is small, counted in bytes of x read.  (Measured, blocks of 32 / of 64,
-// us: d = 2048, E = 64, 2000 tokens 13 / 17, 8192 20 / 25, 16384 26 / 33, 32768 48 / 46, 65536 80 / 68; d = 4096, E = 128,
-// 1000 tokens 12 / 25, 2000 24 / 27, 4096 34 / 32, 8192 53 / 43; E = 256, 1000 tokens 16 / 27, 3000 43 / 35.)
+// us: d = 2048, E = 64, 16384 tokens 27 / 32, 32768 50 / 42, 65536 82 / 63; d = 4096, E = 128, 2000 tokens 24 / 26, 4096
+// 33 / 31, 8192 52 / 39; E = 256, 3000 tokens 43 / 33; d = 1048, E = 100, 8192 tokens 23 / 25.)
 struct GwPlan {
   int mt, tiles, chunks, splits, per_split;
 };
