@@ -222,8 +222,10 @@ class GateTrainer:
 
 
 def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps, lr, token_mask=None):
-    """Fine-tunes gate 0 of `trainer`, starting from w_gate: predictor of `target_scores` from x_now.  Returns the new
-    weights in w_gate's type and the losses of the steps.  The optimizer is PyTorch's Adam on an fp32 copy."""
+    """Fine-tunes the gate of `trainer` (which has one), starting from w_gate: predictor of `target_scores` from x_now.
+    Returns the new weights in w_gate's type and the losses of the steps.  The optimizer is PyTorch's Adam on an fp32 copy."""
+    if trainer.n_gates != 1:      # clip() goes over the gradients of all gates, also those that no step here writes
+        raise ValueError(f"finetune_predictor: a trainer of one gate, not of {trainer.n_gates}")
     w_gate = w_gate.detach()
     master = w_gate.float().clone().requires_grad_(True)
     opt = torch.optim.Adam([master], lr=lr)

@@ -702,6 +702,33 @@ def test_finetuning_runs():
     assert layer.predicted_vs_actual_loads(test, x, x, w)[2] == 1.0
 
 
+@pytest.mark.parametrize("T,E", [(301, 6), (2049, 40), (40001, 8)])
+@pytest.mark.parametrize("start", [1, 7])
+def test_masks_at_any_address(T, E, start):
+    """A mask that begins inside a buffer gives the same bits as an aligned copy of it, whatever lies around it."""
+    k, d = 2, 64
+    rng, scores, idx = tables(T, E, k, 41)
+    mask = mask_of("some", T, 41)
+    around = torch.full((T + 64,), 255, dtype=torch.uint8, device="cuda")
+    inside = around[start:start + T]
+    inside.copy_(dev(mask))
+    s, t, i = dev(scores), dev(rng.standard_normal((T, E)).astype(np.float32)), dev(idx)
+    x, w = torch.from_numpy(rng.standard_normal((T, d))).cuda().bfloat16(), torch.from_numpy(rng.standard_normal((E, d))).cuda().bfloat16()
+    sh = shape_of(T, E, k, 0, d)
+    ws, nb = workspace(sh)
+    results = []
+    for m in (dev(mask), inside):
+        f = lambda *n, dtype=torch.float32: torch.full(n, -7, dtype=dtype, device="cuda")          # noqa: E731
+        out = [f(E, dtype=torch.int32), f(E), f(1), f(1), f(T, E), f(T, E), f(E, d), f(E), f(T, d, dtype=torch.bfloat16)]
+        B.moe_balance_loss(sh, s, i, m, *out[:3], ws, nb)
+        B.moe_gate_distill(sh, s, t, m, 1.0, out[3], out[4], 0, ws, nb)
+        B.moe_route_backward(sh, s, i, s.view(-1)[:T * k], out[0], 0.5, m, out[5], 0)
+        B.moe_gate_backward(sh, x, w, out[4], m, *out[6:], 0, ws, nb)
+        results.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert int(results[0][0].sum()) == int((mask != 0).sum()) * k
+
+
 def test_trainer_takes_nothing_that_does_not_fit():
     T, d, E = 32, 64, 8
     tr = layer.GateTrainer(T, d, E, 2, 1, B.MOE_BF16, 1)
@@ -718,6 +745,8 @@ def test_trainer_takes_nothing_that_does_not_fit():
     model = w.clone().requires_grad_(True)
     new, _ = layer.finetune_predictor(tr, x, target, model, 1, 1e-3)
     assert not new.requires_grad and model.grad is None
+    with pytest.raises(ValueError):
+        layer.finetune_predictor(layer.GateTrainer(T, d, E, 2, 2, B.MOE_BF16, 1), x, target, w, 1, 1e-3)
 
 
 def test_an_empty_batch_gives_zeros_or_leaves_what_is_there():
