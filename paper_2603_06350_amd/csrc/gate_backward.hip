@@ -482,47 +482,51 @@ __global__ __launch_bounds__(GW_THREADS) void gate_weight_wide_kernel(GwArgs a) 
   gate_weight_wide_block<BF16, V>(a, lds, red_b);
 }
 
-// out[i] (+)= the sum of the parts' elements i: four consecutive ones per thread, every fourth part, eight of them on
-// their way at a time; the four sums of an element meet in LDS.  The order of the additions is fixed.
+// out[i] (+)= the sum of the parts' elements i: four consecutive ones per thread, every GROUPS-th part, eight of them on
+// their way at a time; the groups' sums of an element meet in LDS.  The order of the additions is fixed.  Many parts are of
+// few elements and want many groups, few parts large blocks of elements.  (Measured, 2 / 4 / 8 groups, us: 256 parts of 8 x
+// 64 10.3 / 6.1 / 3.9; 64 of 64 x 2048 6.4 / 6.4 / 7.8; 16 of 128 x 4096 6.2 / 9.6 / 6.5.)
 constexpr int GS_THREADS = 256;
-constexpr int GS_GROUPS = 4;
-constexpr int GS_COLUMNS = GS_THREADS / GS_GROUPS;
 __device__ __forceinline__ float4 gs_add(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __device__ __forceinline__ float gs_add(float a, float b) { return a + b; }
-template <class V> __device__ __forceinline__ void gs_column(const V* part, V* out, int64_t n, int64_t i, int splits, int accumulate, V* lds) {
-  const int column = threadIdx.x % GS_COLUMNS, group = threadIdx.x / GS_COLUMNS;
+template <int GROUPS, class V>
+__device__ __forceinline__ void gs_column(const V* part, V* out, int64_t n, int64_t i, int splits, int accumulate, V* lds) {
+  constexpr int COLUMNS = GS_THREADS / GROUPS;
+  const int column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
   V s{};
   if (i < n) {
-    for (int p = group; p < splits; p += 8 * GS_GROUPS) {
+    for (int p = group; p < splits; p += 8 * GROUPS) {
       V v[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         v[u] = V{};
-        if (p + u * GS_GROUPS < splits) v[u] = part[(p + u * GS_GROUPS) * n + i];
+        if (p + u * GROUPS < splits) v[u] = part[(p + u * GROUPS) * n + i];
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) s = gs_add(s, v[u]);
     }
   }
-  if (group > 0) lds[(group - 1) * GS_COLUMNS + column] = s;
+  if (group > 0) lds[(group - 1) * COLUMNS + column] = s;
   __syncthreads();
   if (group == 0 && i < n) {
 #pragma unroll
-    for (int u = 0; u < GS_GROUPS - 1; ++u) s = gs_add(s, lds[u * GS_COLUMNS + column]);
+    for (int u = 0; u < GROUPS - 1; ++u) s = gs_add(s, lds[u * COLUMNS + column]);
     out[i] = accumulate ? gs_add(s, out[i]) : s;
   }
 }
 // Blocks: the first blocks_w for d_w_gate (n elements), the others for d_gate_bias.
+template <int GROUPS>
 __global__ __launch_bounds__(GS_THREADS) void gate_sum_kernel(const float* __restrict__ part_w, float* __restrict__ out_w, int64_t n,
                                                               int blocks_w, const float* __restrict__ part_b,
                                                               float* __restrict__ out_b, int E, int splits, int accumulate) {
-  __shared__ float4 lds[(GS_GROUPS - 1) * GS_COLUMNS];
-  const int column = threadIdx.x % GS_COLUMNS, block = blockIdx.x;
+  constexpr int COLUMNS = GS_THREADS / GROUPS;
+  __shared__ float4 lds[(GROUPS - 1) * COLUMNS];
+  const int column = threadIdx.x % COLUMNS, block = blockIdx.x;
   if (block < blocks_w)
-    gs_column(reinterpret_cast<const float4*>(part_w), reinterpret_cast<float4*>(out_w), n / 4,
-              static_cast<int64_t>(block) * GS_COLUMNS + column, splits, accumulate, lds);
+    gs_column<GROUPS>(reinterpret_cast<const float4*>(part_w), reinterpret_cast<float4*>(out_w), n / 4,
+              static_cast<int64_t>(block) * COLUMNS + column, splits, accumulate, lds);
   else
-    gs_column(part_b, out_b, static_cast<int64_t>(E), static_cast<int64_t>(block - blocks_w) * GS_COLUMNS + column, splits, accumulate,
+    gs_column<GROUPS>(part_b, out_b, static_cast<int64_t>(E), static_cast<int64_t>(block - blocks_w) * COLUMNS + column, splits, accumulate,
               reinterpret_cast<float*>(lds));
 }
 
@@ -823,10 +827,12 @@ static int gate_backward(const moe_shape_t* s, const void* x, const void* w_gate
     }
   }
   if (with_w && parts) {
-    const int blocks_w = d_w_gate ? static_cast<int>((n / 4 + GS_COLUMNS - 1) / GS_COLUMNS) : 0;
-    const int blocks_b = d_gate_bias ? (s->E + GS_COLUMNS - 1) / GS_COLUMNS : 0;
-    hipLaunchKernelGGL(gate_sum_kernel, dim3(static_cast<unsigned>(blocks_w + blocks_b)), dim3(GS_THREADS), 0, st, part, d_w_gate, n,
-                       blocks_w, part_b, d_gate_bias, s->E, p.splits, acc_w);
+    const int columns = GS_THREADS / (p.splits > 64 ? 8 : 2);
+    const int blocks_w = d_w_gate ? static_cast<int>((n / 4 + columns - 1) / columns) : 0;
+    const int blocks_b = d_gate_bias ? (s->E + columns - 1) / columns : 0;
+    const auto kernel = p.splits > 64 ? gate_sum_kernel<8> : gate_sum_kernel<2>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks_w + blocks_b)), dim3(GS_THREADS), 0, st, part, d_w_gate, n, blocks_w, part_b,
+                       d_gate_bias, s->E, p.splits, acc_w);
   }
   return launch_status();
 }
