@@ -97,24 +97,34 @@ template <int G, bool VEC> __device__ __forceinline__ void gl_store(float* __res
 }
 
 // The exponents c (s - m) of a row with the maximum m.  Where c m could pass the largest number (scores of the type's lowest
-// value) m is subtracted first; m = -inf: every s is, and so are the exponents.
-__device__ __forceinline__ void gl_exponents(const float (&s)[4], float m, float (&t)[4]) {
+// value) m is subtracted first; m = -inf: every s is, and so are the exponents.  Returns m's own exponent, what is left of c m.
+__device__ __forceinline__ float gl_exponents(const float (&s)[4], float m, float (&t)[4]) {
   const bool far = fabsf(m) > 1e30f;
-  float scaled = GL_LOG2E * m;
+  float scaled = GL_LOG2E * m, top = m;
 #pragma unroll
   for (int j = 0; j < 4; ++j) t[j] = s[j];
   if (__any(far)) {                                  // rarely
     const float shift = far && m > -INFINITY ? m : 0.f;
     scaled = far ? 0.f : scaled;
+    top -= shift;
 #pragma unroll
     for (int j = 0; j < 4; ++j) t[j] -= shift;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) t[j] = fmaf(GL_LOG2E, t[j], -scaled);
+  return fmaf(GL_LOG2E, top, -scaled);
 }
 
-// 1 / v for a sum of powers, one of which is 1: v_rcp_f32, off by 2^-23 at most.
-__device__ __forceinline__ float gl_inverse(float v) { return __builtin_amdgcn_rcpf(v); }
+// The powers v divided by their sum, zeros where there is none: v_rcp_f32 and a step of correction, so that what is alone in
+// its sum becomes 1.
+__device__ __forceinline__ void gl_divide(float (&v)[4], float sum, bool some) {
+  const float inv = some ? __builtin_amdgcn_rcpf(sum) : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float q = v[j] * inv;
+    v[j] = fmaf(fmaf(-q, sum, v[j]), inv, q);
+  }
+}
 
 // p = softmax of a row, zeros where every score is -inf.  log2p: its logarithms (of base 2).  Returns whether anything
 // is left of the row.
@@ -122,15 +132,14 @@ template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4],
   const float m = gl_max<G>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
   const bool some = m > -INFINITY;
   float t[4];
-  gl_exponents(s, m, t);
+  const float top = gl_exponents(s, m, t);
 #pragma unroll
   for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(t[j]);
   const float sum = gl_sum<G>((p[0] + p[1]) + (p[2] + p[3]));
-  const float inv = some ? gl_inverse(sum) : 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) p[j] *= inv;
+  gl_divide(p, sum, some);
   if (log2p) {
-    const float log2sum = __builtin_amdgcn_logf(some ? sum : 1.f);
+    // the logarithm of a sum of one power is its exponent
+    const float log2sum = sum == __builtin_amdgcn_exp2f(top) ? top : __builtin_amdgcn_logf(some ? sum : 1.f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) (*log2p)[j] = t[j] - log2sum;
   }
@@ -458,9 +467,7 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
             sum += times[j] * v[j];
           }
           sum = gl_sum<G>(sum);
-          const float inv = m > -INFINITY ? gl_inverse(sum) : 0.f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] *= inv;
+          gl_divide(v, sum, m > -INFINITY);
           const float dot = gl_sum<G>((v[0] * g[0] + v[1] * g[1]) + (v[2] * g[2] + v[3] * g[3]));
 #pragma unroll
           for (int j = 0; j < 4; ++j) {

@@ -209,6 +209,30 @@ def test_even_loads_have_no_balance_gradient(E):
     assert not out.np().any()
 
 
+@pytest.mark.parametrize("E,k,renorm", [(1, 1, 0), (1, 1, 1), (8, 1, 1), (64, 1, 1), (250, 1, 1)])
+def test_weights_that_are_always_one_have_no_gradient(E, k, renorm):
+    rng, scores, idx = tables(500, E, k, 8, spread=5.0)
+    out = Guarded((500, E))
+    dw = dev(rng.standard_normal((500, k)).astype(np.float32))
+    B.moe_route_backward(shape_of(500, E, k, renorm), dev(scores), dev(idx), dw, None, 0.0, None, out.t)
+    assert not out.np().any()
+
+
+@pytest.mark.parametrize("E", [1, 7, 64, 256])
+def test_one_expert_left_is_no_loss(E):
+    """Every token has one expert that is not switched off, the same in both gates: probabilities of exactly 1."""
+    rng = np.random.default_rng([9, E])
+    only = rng.integers(0, E, 400)
+    scores, target = (np.full((400, E), -np.inf, dtype=np.float32) for _ in range(2))
+    scores[np.arange(400), only] = 7 * rng.standard_normal(400)
+    target[np.arange(400), only] = 7 * rng.standard_normal(400)
+    sh = shape_of(400, E, 1)
+    ws, nb = workspace(sh)
+    loss, out = Guarded((1,)), Guarded((400, E))
+    B.moe_gate_distill(sh, dev(scores), dev(target), None, 1.0, loss.t, out.t, 0, ws, nb)
+    assert loss.np()[0] == 0.0 and not out.np().any()
+
+
 @pytest.mark.parametrize("E,k", [(9, 3), (13, 4), (16, 4), (36, 9), (50, 16), (100, 7), (250, 64)])
 @pytest.mark.parametrize("renorm", [0, 1])
 def test_route_backward_of_a_few_odd_choices(E, k, renorm):
