@@ -16,9 +16,10 @@
 //     V column tiles: tile i holds the columns V c + i of the lanes c = 0..15.  x (reduction over tokens) and w_gate
 //     (reduction over experts) need no LDS and no transposed copy, and the V results of a lane are V consecutive
 //     columns again: 16-byte stores;
-//   - d_scores (fp32) enters in bf16 pieces: three that hold all its 24 bits for the weights' gradient, which is
-//     stored in fp32; two (16 bits, 2^-16 of each term) for the d_x of bf16 layers, which is rounded to 8 bits.
-//     fp32 layers cut x and w_gate into three pieces as well and leave out the products below 2^-22 of a term.
+//   - d_scores (fp32) enters in three bf16 pieces that hold all its 24 bits.  (Two would do for a d_x that is rounded to
+//     8 bits only where the terms of a sum do not cancel: rows of d_scores add up to nothing, so what gate rows have
+//     in common does.  Measured for d_x, two / three, us: 65536 tokens, d = 2048, E = 64 52 / 51; 16384, d = 4096, E = 128
+//     39 / 48; 8000, d = 5120, E = 250 54 / 63.)  fp32 layers cut x and w_gate into three pieces as well and leave out the products below 2^-22 of a term.
 #include "moe_internal.h"
 
 namespace moe {
@@ -134,15 +135,14 @@ template <bool BF16, int V> __device__ __forceinline__ void gb_transpose(const G
   }
 }
 
-// acc[i] += the products of the pieces of an fp32 operand (TWO: without the last) with those of column tile i, the small
-// ones first.  Products with the same sum are V instructions apart: one that follows directly waits for the sum.
-template <bool BF16, bool TWO, int V>
+// acc[i] += the products of the pieces of an fp32 operand with those of column tile i, the small ones first.  Products with the same sum are V instructions apart: one that follows directly waits for the sum.
+template <bool BF16, int V>
 __device__ __forceinline__ void gb_products(uint4 h, uint4 m, uint4 l, const GbFrag<BF16, V>& b, gb_f32x4 (&acc)[V]) {
   auto step = [&](uint4 a, const uint4 (&f)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = gb_mfma(a, f[i], acc[i]);
   };
-  if constexpr (!TWO) step(l, b.f[0]);
+  step(l, b.f[0]);
   if constexpr (!BF16) step(h, b.f[2]);
   if constexpr (!BF16) step(m, b.f[1]);
   step(m, b.f[0]);
@@ -256,7 +256,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
     load(t0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) gb_products<BF16, false, V>(p[m][0], p[m][1], p[m][2], b, acc[m]);
+    for (int m = 0; m < MT; ++m) gb_products<BF16, V>(p[m][0], p[m][1], p[m][2], b, acc[m]);
   }
 
   // sums of the waves, 16 experts at a time: lane 16 g + c of a wave holds experts 4 g + 0..3 of the columns V c + i
@@ -415,7 +415,7 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
 #pragma unroll
       for (int q = 0; q < 3; ++q)
         p[q] = *reinterpret_cast<const uint4*>(lds + at_lds + (half * 3 + q) * GWW_PIECES + (m * MOE_WAVE + lane) * 16);
-      gb_products<BF16, false, V>(p[0], p[1], p[2], b, acc[m]);
+      gb_products<BF16, V>(p[0], p[1], p[2], b, acc[m]);
     }
     at_lds = next;
   }
@@ -548,7 +548,7 @@ struct GxArgs {
 
 // THREADS: 256, or 512 for two groups of waves side by side, each with GT tokens of a step of its own.
 template <bool BF16, int KS, int THREADS> struct GxTile {
-  static constexpr int P = BF16 ? 2 : 3;             // pieces of d_scores
+  static constexpr int P = 3;                        // pieces of d_scores
   static constexpr int GT = KS <= 2 ? 64 : 128 / KS; // tokens of a wave's step
   static constexpr int STEP = GT * THREADS / 256;    // tokens of the block's step
   static constexpr int CPT = 8 * KS;                 // chunks of four experts of a token
@@ -648,8 +648,9 @@ __device__ __forceinline__ void gate_x_block(const GxArgs& a, int block, unsigne
         uint4 q[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) q[p] = *reinterpret_cast<const uint4*>(lds + (buf * P + p) * PIECE + at);
-        gb_products<BF16, BF16, V>(q[0], q[1], q[P - 1], w[k], acc);
+        gb_products<BF16, V>(q[0], q[1], q[2], w[k], acc);
       }
+      __builtin_amdgcn_sched_barrier(0);               // (with the next tokens' operands on top of these, registers spill)
       uint32_t keep = 0x01010101u;                   // padded tokens: zeros, or nothing where d_x is added to
       if constexpr (ACC) keep = reals[buf * (STEP / 4) + first / 4 + 4 * m + g];
 #pragma unroll

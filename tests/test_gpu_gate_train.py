@@ -825,3 +825,26 @@ def test_tensors_that_do_not_fit_are_refused():
     # the same gradient may be read twice
     lst = B.GradList([scores, scores], [f(T, E), f(T, E)])
     assert len(lst) == 2
+
+
+# ------------------------------------------------------------------------------------------------ products of few terms
+@pytest.mark.parametrize("T,d,E", [(257, 136, 8), (300, 264, 24), (3000, 520, 64), (129, 512, 100), (65, 1048, 200)])
+@pytest.mark.parametrize("dtype", [B.MOE_BF16, B.MOE_F32])
+def test_d_x_of_terms_that_cancel(T, d, E, dtype):
+    """Two experts of a token with nearly opposite gradients, and gate rows with a common part: what is left is small
+    beside its two terms, whose 24 bits have to be in it: (2 + 8) 2u of the terms' sizes, and one rounding to storage."""
+    rng = np.random.default_rng([55, T, E])
+    w = store(1.0 + 0.03 * rng.standard_normal((E, d)), dtype)
+    ds = np.zeros((T, E), dtype=np.float32)
+    pick = np.stack([rng.permutation(E)[:2] for _ in range(T)])
+    a = (rng.random(T) + 0.5).astype(np.float32)
+    ds[np.arange(T), pick[:, 0]] = a
+    ds[np.arange(T), pick[:, 1]] = -a * (1 + 0.03 * rng.standard_normal(T)).astype(np.float32)
+    sh = shape_of(T, E, 1, 0, d, dtype)
+    dx = Guarded((T, d), torch.float32 if dtype == B.MOE_F32 else torch.bfloat16)
+    B.moe_gate_backward(sh, None, layer.to_device(w), dev(ds), None, None, None, dx.t, 0, None, 0)
+    w64 = orc.to_f64(w)
+    ref, size = ds.astype(np.float64) @ w64, np.abs(ds.astype(np.float64)) @ np.abs(w64)
+    half = U if dtype == B.MOE_F32 else 2.0 ** -8
+    err, tol = np.abs(dx.np() - ref), half * np.abs(ref) + (1 + half) * 20 * U * size
+    assert (err <= tol).all(), f"{(err > tol).mean():.4f} of the elements, {(err / size).max() / U:.1f} u of the terms"
