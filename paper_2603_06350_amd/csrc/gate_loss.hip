@@ -13,7 +13,8 @@
 // time, 1 KiB in one piece, whatever E is, and the sums over a row take log2(G) steps between lanes.
 //
 // Powers are taken of 2: with m the row's maximum and c = log2(e), e^(s-m) = 2^(c s - c m) is one fused multiply-add
-// (rounded once) and one v_exp_f32.  The rounding of c m is the same for a whole row and divides out of p.
+// (rounded once) and one v_exp_f32.  The rounding of c m is the same for a whole row and divides out of p, as long as
+// it is small: from |m| of some 1e9 on it is more than what a power of 2 can hold (GL_FAR).
 #include <type_traits>
 
 #include "moe_internal.h"
@@ -96,10 +97,11 @@ template <int G, bool VEC> __device__ __forceinline__ void gl_store(float* __res
   }
 }
 
-// The exponents c (s - m) of a row with the maximum m.  Where c m could pass the largest number (scores of the type's lowest
-// value) m is subtracted first; m = -inf: every s is, and so are the exponents.  Returns m's own exponent, what is left of c m.
+// The exponents c (s - m) of a row with the maximum m.  Beyond GL_FAR, up to which the rounding of c m is 2^-8 at most, m is
+// subtracted first; m = -inf: every s is, and so are the exponents.  Returns m's own exponent, what is left of c m.
+constexpr float GL_FAR = 65536.f;
 __device__ __forceinline__ float gl_exponents(const float (&s)[4], float m, float (&t)[4]) {
-  const bool far = fabsf(m) > 1e30f;
+  const bool far = fabsf(m) > GL_FAR;
   float scaled = GL_LOG2E * m, top = m;
 #pragma unroll
   for (int j = 0; j < 4; ++j) t[j] = s[j];

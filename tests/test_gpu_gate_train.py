@@ -848,3 +848,90 @@ def test_d_x_of_terms_that_cancel(T, d, E, dtype):
     half = U if dtype == B.MOE_F32 else 2.0 ** -8
     err, tol = np.abs(dx.np() - ref), half * np.abs(ref) + (1 + half) * 20 * U * size
     assert (err <= tol).all(), f"{(err > tol).mean():.4f} of the elements, {(err / size).max() / U:.1f} u of the terms"
+
+
+# ------------------------------------------------------------------------------------------------ scores of any size
+def shifted(scores):
+    """Rows less their maximum, cut at -104, below which e^s is no fp32 number: the same probabilities to within 1e-45."""
+    s = np.asarray(scores, dtype=np.float64)
+    m = s.max(axis=1, keepdims=True)
+    return np.maximum(s - np.where(np.isneginf(m), 0.0, m), -104.0)
+
+
+def check_losses_of_large_scores(scores, target, idx, mask=None):
+    """The three calls on a table whose rows' maxima may have any size.  Tolerances as above, with the spread of what is not
+    zero in fp32; a term q (log q - log p) of the loss is off by 32 u of its parts' sizes, and its sum over E by 16 u."""
+    T, E = scores.shape
+    k = idx.shape[1]
+    rows = np.arange(T) if mask is None else np.flatnonzero(mask)
+    low = shifted(scores)
+    rng = np.random.default_rng([T, E])
+    dw = rng.standard_normal((T, k)).astype(np.float32)
+    sh = shape_of(T, E, k)
+    ws, nb = workspace(sh)
+    m = dev(mask)
+    counts, prob_sum, loss = Guarded((E,), torch.int32, -77), Guarded((E,)), Guarded((1,))
+    B.moe_balance_loss(sh, dev(scores), dev(idx), m, counts.t, prob_sum.t, loss.t, ws, nb)
+    rc, rp, rl = go.balance_loss(scores, idx, mask)
+    tol = (2 * 104 + 24 + T / 512 + 64) * U
+    assert np.array_equal(counts.np(), rc)
+    assert (np.abs(prob_sum.np() - rp) <= tol * rp + TINY).all(), (prob_sum.np(), rp)
+    assert abs(loss.np()[0] - rl) <= (tol + 2 * U) * abs(rl)
+    for renorm in (0, 1):
+        out = Guarded((T, E))
+        B.moe_route_backward(shape_of(T, E, k, renorm), dev(scores), dev(idx), dev(dw), dev(rc.astype(np.int32)), 0.5 * T, m, out.t)
+        ref = go.route_backward(scores, idx, dw, rc, 0.5 * T, renorm, mask)
+        # (the chosen experts have a maximum of their own: what they are is not what is left of `low`)
+        size = route_bound(low, idx, dw, rc.astype(np.float64), 0.5 * T, 0, mask, k)
+        for j in range(k if renorm else 0):
+            size[rows, idx[rows, j]] += (2 * (208 + 24) + 24 + k) * U * 2 * np.abs(dw[rows]).max(axis=1)
+        err = np.abs(out.np() - ref)
+        assert (err <= size).all(), (renorm, np.argwhere(~(err <= size))[:4], err.max())
+    out, loss = Guarded((T, E)), Guarded((1,))
+    B.moe_gate_distill(sh, dev(scores), dev(target), m, 2.0, loss.t, out.t, 0, ws, nb)
+    rl, rg = go.gate_distill(scores, target, 2.0, mask)
+    p, q = go.softmax(scores), go.softmax(target)
+    err = np.abs(out.np() - rg)
+    assert (err <= (208 + 28) * U * 2.0 / rows.size * (p + q) + TINY).all(), err.max()
+    s64, t64 = scores.astype(np.float64), target.astype(np.float64)
+    log_p = s64 - s64.max(axis=1, keepdims=True) - np.log(np.exp(s64 - s64.max(axis=1, keepdims=True)).sum(axis=1, keepdims=True))
+    log_q = t64 - t64.max(axis=1, keepdims=True) - np.log(np.exp(t64 - t64.max(axis=1, keepdims=True)).sum(axis=1, keepdims=True))
+    size = np.where(q > 0, q * (np.abs(log_p) + np.abs(log_q) + 24), 0.0)[rows].sum() / rows.size
+    assert np.isfinite(rl) and abs(loss.np()[0] - rl) <= 48 * U * size + 2 * U * abs(rl), (loss.np()[0], rl)
+
+
+LARGE = [7e4, 1e6, -1e6, 1e8, -1e8, 1.6e9, 3e9, 5e9, -5e9, 1e10, -1e10, 1e12, 1e20, -1e20, 1e29, -1e29, -1e30, 2e30, -3e38]
+
+
+@pytest.mark.parametrize("E", [4, 7, 64, 200])
+def test_chosen_experts_with_a_switch_off_value(E):
+    """Finite switch-off values: of all chosen experts, of all but one, of all experts."""
+    rng = np.random.default_rng([52, E])
+    for off in (-1e9, -1e10, -1e20, -1e30, -np.finfo(np.float32).max):
+        scores = rng.standard_normal((90, E)).astype(np.float32)
+        idx = np.stack([rng.permutation(E)[:2] for _ in range(90)]).astype(np.int32)
+        scores[np.arange(30), idx[:30, 0]] = off
+        scores[np.arange(30), idx[:30, 1]] = off
+        scores[30:60] = np.where(np.arange(E) == idx[30:60, :1], scores[30:60], off)
+        scores[60:70] = off
+        check_losses_of_large_scores(scores, scores, idx)
+
+
+@pytest.mark.parametrize("E", [1, 6, 8, 64, 250])
+def test_rows_of_large_scores(E):
+    """A batch of ordinary tokens and of tokens whose scores are all alike, or a few steps of fp32 apart, at any size."""
+    rng = np.random.default_rng([51, E])
+    k = min(E, 3)
+    T = 3 * len(LARGE) + 40
+    scores = rng.standard_normal((T, E)).astype(np.float32)
+    for i, v in enumerate(LARGE):
+        scores[3 * i] = v
+        steps = rng.integers(-3, 4, E)
+        scores[3 * i + 1] = np.float32(v) + steps * np.spacing(np.float32(abs(v)))
+        scores[3 * i + 2, rng.random(E) < 0.5] = v
+    target = scores.copy()
+    target[:, 0] += np.float32(0.5)
+    target[::3] = rng.standard_normal((len(target[::3]), E))
+    idx = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    check_losses_of_large_scores(scores, np.where(np.arange(T)[:, None] % 3 == 0, target, scores), idx)
+    check_losses_of_large_scores(target, target, idx, mask_of("some", T, 51))
