@@ -128,9 +128,13 @@ __device__ __forceinline__ void gl_divide(float (&v)[4], float sum, bool some) {
   }
 }
 
-// p = softmax of a row, zeros where every score is -inf.  log2p: its logarithms (of base 2).  Returns whether anything
-// is left of the row.
-template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4], float (&p)[4], float (*log2p)[4] = nullptr) {
+// Logarithms (of base 2) of a row's probabilities, and of the largest, that of the score m.
+struct GlLogs {
+  float p[4], m, top;
+};
+
+// p = softmax of a row, zeros where every score is -inf.  Returns whether anything is left of the row.
+template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4], float (&p)[4], GlLogs* logs = nullptr) {
   const float m = gl_max<G>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
   const bool some = m > -INFINITY;
   float t[4];
@@ -139,11 +143,13 @@ template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4],
   for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(t[j]);
   const float sum = gl_sum<G>((p[0] + p[1]) + (p[2] + p[3]));
   gl_divide(p, sum, some);
-  if (log2p) {
+  if (logs) {
     // the logarithm of a sum of one power is its exponent
     const float log2sum = sum == __builtin_amdgcn_exp2f(top) ? top : __builtin_amdgcn_logf(some ? sum : 1.f);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) (*log2p)[j] = t[j] - log2sum;
+    for (int j = 0; j < 4; ++j) logs->p[j] = t[j] - log2sum;
+    logs->m = m;
+    logs->top = top - log2sum;
   }
   return some;
 }
@@ -530,6 +536,10 @@ __device__ __forceinline__ double gl_tokens(const uint8_t* __restrict__ mask, co
 }
 static_assert(GL_COUNT_BLOCKS == MOE_WAVE, "one part per lane");
 
+struct GlRowPair {
+  float s[4], u[4];
+};
+
 // ACC: d_scores is added to.
 template <int G, bool VEC, bool ACC>
 __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __restrict__ scores, const float* __restrict__ target,
@@ -561,19 +571,42 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
         scale = n > 0.0 ? static_cast<float>(coef / n) : 0.f;
       },
       [&](Row& r, int t, bool there, bool real) {
-        float p[4], q[4], lp[4], lq[4], d[4];
+        float p[4], q[4], d[4];
+        GlLogs lp, lq;
         const bool left_p = gl_softmax<G>(r.s, p, &lp), left_q = gl_softmax<G>(r.u, q, &lq);
         const bool counts = real && left_p && left_q;
         float row = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          row += q[j] > 0.f ? q[j] * (lq[j] - lp[j]) : 0.f;      // q = 0 has no part
+          row += q[j] > 0.f ? q[j] * (lq.p[j] - lp.p[j]) : 0.f;      // q = 0 has no part
           d[j] = counts ? scale * (p[j] - q[j]) : 0.f;
           if constexpr (ACC) d[j] += r.old[j];
         }
         sum += counts ? row : 0.f;
         if (d_scores && there && (real || !ACC)) gl_store<G, VEC>(d_scores, t, E, l, d);
       });
+  if (__any(!(fabs(sum) < INFINITY))) {
+    // rarely: finite scores so far below their row's maximum that the difference, or what it is multiplied by, passes the
+    // largest number.  The wave's rows once more, in 64 bits (in the loop above that costs a single small call 0.5 us of 4.3).
+    sum = 0.0;
+    gl_rows<G, GlRowPair>(
+        rows.n, mask ? mask + rows.begin : nullptr, scores,
+        [&](GlRowPair& r, int t) {
+          gl_load<G, VEC>(scores, t, E, l, -INFINITY, r.s);
+          gl_load<G, VEC>(target, t, E, l, -INFINITY, r.u);
+        },
+        [] {},
+        [&](GlRowPair& r, int, bool, bool real) {
+          float p[4], q[4];
+          GlLogs lp, lq;
+          const bool left_p = gl_softmax<G>(r.s, p, &lp), left_q = gl_softmax<G>(r.u, q, &lq);
+          double row = 0.0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (q[j] > 0.f) row += q[j] * (lq.p[j] - lp.top - (static_cast<double>(r.s[j]) - lp.m) * 1.4426950408889634);
+          sum += real && left_p && left_q ? row : 0.0;
+        });
+  }
   sum = gl_block_sum(sum * GL_LN2, lds);
   if (threadIdx.x != 0) return;
   if (gridDim.x > 1)

@@ -935,3 +935,19 @@ def test_rows_of_large_scores(E):
     idx = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
     check_losses_of_large_scores(scores, np.where(np.arange(T)[:, None] % 3 == 0, target, scores), idx)
     check_losses_of_large_scores(target, target, idx, mask_of("some", T, 51))
+
+
+@pytest.mark.parametrize("E", [2, 5, 64, 130])
+def test_a_target_that_wants_finite_scores_far_below(E):
+    """The loss is finite as long as the scores are: q times a difference that passes the largest fp32 number itself, too."""
+    rng = np.random.default_rng([53, E])
+    T = 40
+    for top, low in ((0.3, -3.4e38), (1.0, -1e38), (2e38, -2e38), (3e38, -3.4e38), (1e20, -1e30)):
+        scores = rng.standard_normal((T, E)).astype(np.float32)
+        target = rng.standard_normal((T, E)).astype(np.float32)
+        scores[5, 0], scores[5, 1] = top, low
+        scores[9] = low
+        scores[9, 1] = top
+        target[[5, 9]] = rng.standard_normal((2, E))
+        target[5, 1] = -2.0
+        check_losses_of_large_scores(scores, target, np.zeros((T, 1), dtype=np.int32))
