@@ -317,7 +317,8 @@ int moe_place_replicas(int32_t E, const int32_t* loads, const int32_t* replicas,
  *   -> moe_gate_backward -> moe_clip_grads over the gradients of all gates -> the caller's optimizer.
  * Common to the calls below:
  *   scores      [T,E] fp32, the scores_out of moe_route.  A score of -inf is an expert that is switched off:
- *               probability 0; a token with no expert left has probabilities 0 and gets no gradient.
+ *               probability 0; a token with no expert left has probabilities 0 and gets no gradient.  A NaN among
+ *               the scores of a token that counts makes NaN of what its probabilities enter.
  *   token_mask  [T] bytes, 0 = a padded token, or NULL (all tokens count).  Padded tokens add nothing to any sum and
  *               their gradients are 0; nothing else that belongs to them is used, whatever it holds.
  *   accumulate  gradients are added to what the output holds (a padded token's is then left as it was); 0: written

@@ -133,15 +133,16 @@ struct GlLogs {
   float p[4], m, top;
 };
 
-// p = softmax of a row, zeros where every score is -inf.  Returns whether anything is left of the row.
+// p = softmax of a row, zeros where every score is -inf, NaN where one is NaN (which a maximum does not show).  Returns
+// whether anything is left of the row.
 template <int G> __device__ __forceinline__ bool gl_softmax(const float (&s)[4], float (&p)[4], GlLogs* logs = nullptr) {
   const float m = gl_max<G>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
-  const bool some = m > -INFINITY;
   float t[4];
   const float top = gl_exponents(s, m, t);
 #pragma unroll
   for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(t[j]);
   const float sum = gl_sum<G>((p[0] + p[1]) + (p[2] + p[3]));
+  const bool some = sum != 0.f;
   gl_divide(p, sum, some);
   if (logs) {
     // the logarithm of a sum of one power is its exponent
@@ -475,7 +476,7 @@ __global__ __launch_bounds__(GL_THREADS) void route_backward_kernel(const float*
             sum += times[j] * v[j];
           }
           sum = gl_sum<G>(sum);
-          gl_divide(v, sum, m > -INFINITY);
+          gl_divide(v, sum, sum != 0.f);
           const float dot = gl_sum<G>((v[0] * g[0] + v[1] * g[1]) + (v[2] * g[2] + v[3] * g[3]));
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -578,7 +579,7 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
         float row = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          row += q[j] > 0.f ? q[j] * (lq.p[j] - lp.p[j]) : 0.f;      // q = 0 has no part
+          row += q[j] != 0.f ? q[j] * (lq.p[j] - lp.p[j]) : 0.f;     // q = 0 has no part
           d[j] = counts ? scale * (p[j] - q[j]) : 0.f;
           if constexpr (ACC) d[j] += r.old[j];
         }
@@ -603,7 +604,7 @@ __global__ __launch_bounds__(GL_THREADS) void distill_kernel(const float* __rest
           double row = 0.0;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (q[j] > 0.f) row += q[j] * (lq.p[j] - lp.top - (static_cast<double>(r.s[j]) - lp.m) * 1.4426950408889634);
+            if (q[j] != 0.f) row += q[j] * (lq.p[j] - lp.top - (static_cast<double>(r.s[j]) - lp.m) * 1.4426950408889634);
           sum += real && left_p && left_q ? row : 0.0;
         });
   }

@@ -951,3 +951,29 @@ def test_a_target_that_wants_finite_scores_far_below(E):
         target[[5, 9]] = rng.standard_normal((2, E))
         target[5, 1] = -2.0
         check_losses_of_large_scores(scores, target, np.zeros((T, 1), dtype=np.int32))
+
+
+@pytest.mark.parametrize("E", [1, 6, 64, 129])
+@pytest.mark.parametrize("where", ["all scores", "one score", "scores beside -inf", "one target", "all targets"])
+def test_nan_scores_of_a_token_that_counts_are_seen(E, where):
+    """A NaN makes the loss and the token's own gradient NaN; it is not taken for a token with no expert left."""
+    rng = np.random.default_rng([54, E])
+    T = 70
+    scores, target = (rng.standard_normal((T, E)).astype(np.float32) for _ in range(2))
+    table = scores if "score" in where else target
+    if where.startswith("all"):
+        table[11] = np.nan
+    else:
+        if "beside" in where:
+            table[11] = -np.inf
+        table[11, E // 2] = np.nan
+    sh = shape_of(T, E, 1)
+    ws, nb = workspace(sh)
+    loss, out = Guarded((1,)), Guarded((T, E))
+    B.moe_gate_distill(sh, dev(scores), dev(target), None, 1.0, loss.t, out.t, 0, ws, nb)
+    got = out.np()
+    assert np.isnan(loss.np()[0]) and np.isnan(got[11]).all()
+    assert np.isfinite(np.delete(got, 11, axis=0)).all()
+    mask = np.ones(T, dtype=np.uint8)
+    mask[11] = 0
+    check_distill(T, E, mask, np.where(np.isnan(scores), 0, scores), np.where(np.isnan(target), 0, target), 1.0, 0)
