@@ -134,12 +134,13 @@ __global__ __launch_bounds__(GR_THREADS) void grad_finish_kernel(const double* _
   if (threadIdx.x == 0) *norm = static_cast<float>(s);
 }
 
-template <bool BF16> __device__ __forceinline__ void grad_scale(const GradPiece& g, float c) {
+template <bool BF16, class C> __device__ __forceinline__ void grad_scale(const GradPiece& g, C c) {
+  auto times = [&](float v) { return static_cast<float>(v * c); };
   auto one = [&](int64_t i) {
     if constexpr (BF16)
-      static_cast<bf16_t*>(g.out)[i] = f32_to_bf16(bf16_to_f32(static_cast<const bf16_t*>(g.data)[i]) * c);
+      static_cast<bf16_t*>(g.out)[i] = f32_to_bf16(times(bf16_to_f32(static_cast<const bf16_t*>(g.data)[i])));
     else
-      static_cast<float*>(g.out)[i] = static_cast<const float*>(g.data)[i] * c;
+      static_cast<float*>(g.out)[i] = times(static_cast<const float*>(g.data)[i]);
   };
   if ((reinterpret_cast<uintptr_t>(g.out) ^ reinterpret_cast<uintptr_t>(g.data)) & 15) {   // no common alignment
     for (int64_t i = g.begin + threadIdx.x; i < g.end; i += GR_THREADS) one(i);
@@ -151,7 +152,7 @@ template <bool BF16> __device__ __forceinline__ void grad_scale(const GradPiece&
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          w[k] = BF16 ? pack_bf16x2(bf16lo(w[k]) * c, bf16hi(w[k]) * c) : __float_as_uint(__uint_as_float(w[k]) * c);
+          w[k] = BF16 ? pack_bf16x2(times(bf16lo(w[k])), times(bf16hi(w[k]))) : __float_as_uint(times(__uint_as_float(w[k])));
         nt_store(reinterpret_cast<uint4*>(static_cast<char*>(g.out) + i * (BF16 ? 2 : 4)), make_uint4(w[0], w[1], w[2], w[3]));
       },
       one);
@@ -167,15 +168,22 @@ __global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable tab, i
   const double s = grad_total_norm(part, pieces, lds);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(s);
   // 1 where `norm`, which the caller sees, is no finite number
-  const float c = s > max_norm && static_cast<float>(s) < INFINITY ? static_cast<float>(max_norm / s) : 1.f;
+  const double exact = s > max_norm && static_cast<float>(s) < INFINITY ? max_norm / s : 1.0;
+  const float c = static_cast<float>(exact);
   const int b = (gridDim.x / 8 - 1 - blockIdx.x / 8) * 8 + blockIdx.x % 8;
   if (b >= blocks) return;
   const GradPiece g = grad_piece(tab, count, piece, b);
   if (c == 1.f && g.out == g.data) return;
-  if (g.bf16)
+  if (exact > 0.0 && exact < 0x1p-126) {             // few bits of it, or none, are left in 32
+    if (g.bf16)
+      grad_scale<true>(g, exact);
+    else
+      grad_scale<false>(g, exact);
+  } else if (g.bf16) {
     grad_scale<true>(g, c);
-  else
+  } else {
     grad_scale<false>(g, c);
+  }
 }
 
 static int check_grads(int32_t count, const moe_tensor_t* tensors, bool with_out) {

@@ -977,3 +977,12 @@ def test_nan_scores_of_a_token_that_counts_are_seen(E, where):
     mask = np.ones(T, dtype=np.uint8)
     mask[11] = 0
     check_distill(T, E, mask, np.where(np.isnan(scores), 0, scores), np.where(np.isnan(target), 0, target), 1.0, 0)
+
+
+def test_clip_grads_by_factors_below_the_normal_numbers():
+    """max_norm / norm is a number of few bits in fp32, or none, where the scaled gradients are ordinary numbers."""
+    for value, share in ((1e35, 1e-39), (1e35, 3e-44), (1e36, 1e-45), (7e36, 7e-47)):
+        g = [torch.full((1000,), value, dtype=torch.float32, device="cuda"), torch.full((77,), -value, dtype=torch.bfloat16, device="cuda")]
+        check_clip([t.clone() for t in g], share)
+        check_clip([t.clone() for t in g], share, in_place=True)
+        check_clip([t.clone() for t in g], share, out_offset=1)
