@@ -378,7 +378,8 @@ int moe_gate_distill(const moe_shape_t* shape, const float* scores, const float*
  * At least one of them.  x is used for d_w_gate only, w_gate for d_x only (else they may be NULL), the workspace for
  * d_w_gate and d_gate_bias.  accumulate: 0, or a sum of MOE_ACCUMULATE_WEIGHTS (d_w_gate and d_gate_bias: micro-batches)
  * and MOE_ACCUMULATE_X (d_x: next to what the experts' gradients left there).  Rows of x of at most 16 MiB (else
- * MOE_ERR_UNSUPPORTED).
+ * MOE_ERR_UNSUPPORTED).  Sums are fp32, terms are not rounded (numbers below 2^-109 may lose low bits); an infinity among
+ * them gives NaN.
  */
 #define MOE_ACCUMULATE_WEIGHTS 1
 #define MOE_ACCUMULATE_X 2

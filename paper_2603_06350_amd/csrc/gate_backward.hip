@@ -19,7 +19,10 @@
 //   - d_scores (fp32) enters in three bf16 pieces that hold all its 24 bits.  (Two would do for a d_x that is rounded to
 //     8 bits only where the terms of a sum do not cancel: rows of d_scores add up to nothing, so what gate rows have
 //     in common does.  Measured for d_x, two / three, us: 65536 tokens, d = 2048, E = 64 52 / 51; 16384, d = 4096, E = 128
-//     39 / 48; 8000, d = 5120, E = 250 54 / 63.)  fp32 layers cut x and w_gate into three pieces as well and leave out the products below 2^-22 of a term.
+//     39 / 48; 8000, d = 5120, E = 250 54 / 63.)  fp32 layers cut x and w_gate into three pieces as well and multiply
+//     eight of the nine products (gb_products), so that a sum of one product is as good as rounded: within 1.02 x 2^-24 of
+//     it.  (Six products and one sum for all, which leave up to 5 x 2^-24, us: 8192 tokens, d = 2048, E = 8 27.4, with eight
+//     29; 40000, d = 1024, E = 64 80 and 87; 8000, d = 4096, E = 128 104 and 123; 8000, d = 1024, E = 256 58 and 67.)
 #include "moe_internal.h"
 
 namespace moe {
@@ -135,19 +138,37 @@ template <bool BF16, int V> __device__ __forceinline__ void gb_transpose(const G
   }
 }
 
-// acc[i] += the products of the pieces of an fp32 operand with those of column tile i, the small ones first.  Products with the same sum are V instructions apart: one that follows directly waits for the sum.
+// acc[i] += the products of the pieces of an fp32 operand with those of column tile i, the small ones first.  Products with
+// the same sum are V instructions apart: one that follows directly waits for the sum.  fp32 layers: without the product of
+// the last pieces, 2^-31 of the whole or less; the matrix instruction does not round its sum to nearest, so all but
+// the leading products, 2^-6 of them and less, have sums of their own, `low`, that the caller adds (gb_add).
+template <bool BF16, int V> using GbLow = gb_f32x4[BF16 ? 1 : V];
 template <bool BF16, int V>
-__device__ __forceinline__ void gb_products(uint4 h, uint4 m, uint4 l, const GbFrag<BF16, V>& b, gb_f32x4 (&acc)[V]) {
-  auto step = [&](uint4 a, const uint4 (&f)[V]) {
+__device__ __forceinline__ void gb_products(uint4 h, uint4 m, uint4 l, const GbFrag<BF16, V>& b, gb_f32x4 (&acc)[V], GbLow<BF16, V>& low) {
+  auto step = [&](uint4 a, const uint4 (&f)[V], gb_f32x4 (&to)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = gb_mfma(a, f[i], acc[i]);
+    for (int i = 0; i < V; ++i) to[i] = gb_mfma(a, f[i], to[i]);
   };
-  step(l, b.f[0]);
-  if constexpr (!BF16) step(h, b.f[2]);
-  if constexpr (!BF16) step(m, b.f[1]);
-  step(m, b.f[0]);
-  if constexpr (!BF16) step(h, b.f[1]);
-  step(h, b.f[0]);
+  if constexpr (BF16) {
+    step(l, b.f[0], acc);
+    step(m, b.f[0], acc);
+    step(h, b.f[0], acc);
+  } else {
+    step(l, b.f[1], low);
+    step(m, b.f[2], low);
+    step(l, b.f[0], low);
+    step(h, b.f[2], low);
+    step(h, b.f[0], acc);
+    step(m, b.f[1], low);
+    step(m, b.f[0], low);
+    step(h, b.f[1], low);
+  }
+}
+template <bool BF16, int V> __device__ __forceinline__ void gb_add(gb_f32x4 (&acc)[V], const GbLow<BF16, V>& low) {
+  if constexpr (!BF16) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] += low[i];
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ weights' gradient
@@ -256,7 +277,11 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
     load(t0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) gb_products<BF16, V>(p[m][0], p[m][1], p[m][2], b, acc[m]);
+    for (int m = 0; m < MT; ++m) {
+      GbLow<BF16, V> low = {};
+      gb_products<BF16, V>(p[m][0], p[m][1], p[m][2], b, acc[m], low);
+      gb_add<BF16, V>(acc[m], low);
+    }
   }
 
   // sums of the waves, 16 experts at a time: lane 16 g + c of a wave holds experts 4 g + 0..3 of the columns V c + i
@@ -415,7 +440,9 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
 #pragma unroll
       for (int q = 0; q < 3; ++q)
         p[q] = *reinterpret_cast<const uint4*>(lds + at_lds + (half * 3 + q) * GWW_PIECES + (m * MOE_WAVE + lane) * 16);
-      gb_products<BF16, V>(p[0], p[1], p[2], b, acc[m]);
+      GbLow<BF16, V> low = {};
+      gb_products<BF16, V>(p[0], p[1], p[2], b, acc[m], low);
+      gb_add<BF16, V>(acc[m], low);
     }
     at_lds = next;
   }
@@ -641,6 +668,7 @@ __device__ __forceinline__ void gate_x_block(const GxArgs& a, int block, unsigne
       gb_f32x4 acc[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) acc[i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
+      GbLow<BF16, V> low = {};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         // lane 16 g + c: experts 32 k + 8 g + 0..7 of token 16 m + c of this wave's
@@ -648,8 +676,9 @@ __device__ __forceinline__ void gate_x_block(const GxArgs& a, int block, unsigne
         uint4 q[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) q[p] = *reinterpret_cast<const uint4*>(lds + (buf * P + p) * PIECE + at);
-        gb_products<BF16, V>(q[0], q[1], q[2], w[k], acc);
+        gb_products<BF16, V>(q[0], q[1], q[2], w[k], acc, low);
       }
+      gb_add<BF16, V>(acc, low);
       __builtin_amdgcn_sched_barrier(0);               // (with the next tokens' operands on top of these, registers spill)
       uint32_t keep = 0x01010101u;                   // padded tokens: zeros, or nothing where d_x is added to
       if constexpr (ACC) keep = reals[buf * (STEP / 4) + first / 4 + 4 * m + g];
@@ -676,9 +705,10 @@ __device__ __forceinline__ void gate_x_block(const GxArgs& a, int block, unsigne
   }
 }
 
-// A launch of its own (launch_narrow says when 17 to 32 experts have one; more always do).
+// A launch of its own (launch_narrow says when 17 to 32 experts have one; more always do).  Two blocks to a CU, also
+// where that spills a few registers: fp32 layers of 200 experts, 2000 tokens, d = 4096 33.6 us instead of 42 with one.
 template <bool BF16, int KS, int V, bool WHOLE, bool ACC>
-__global__ __launch_bounds__(256, KS < 8 ? 2 : 1) void gate_x_kernel(GxArgs a) {
+__global__ __launch_bounds__(256, 2) void gate_x_kernel(GxArgs a) {
   using Tile = GxTile<BF16, KS, 256>;
   __shared__ __align__(16) unsigned char lds[Tile::LDS];
   __shared__ uint32_t reals[Tile::STEP / 2];
@@ -686,9 +716,10 @@ __global__ __launch_bounds__(256, KS < 8 ? 2 : 1) void gate_x_kernel(GxArgs a) {
 }
 
 // Up to 32 experts, where either gradient's blocks leave room for the other's: both in one launch, eight blocks of the one
-// and eight of the other in turn (one per XCD each), so that x is read while d_x is written.
+// and eight of the other in turn (one per XCD each), so that x is read while d_x is written.  (Two blocks to a CU up to 16
+// experts of bf16 layers; fp32 layers' pieces would spill: 8192 tokens, d = 2048, E = 8 34 us instead of 29.)
 template <bool BF16, int MT, bool WHOLE, bool ACC>
-__global__ __launch_bounds__(GW_THREADS, MT == 1 && !ACC ? 4 : 2) void gate_narrow_kernel(GwArgs w, int blocks_w, GxArgs x, int blocks_x) {
+__global__ __launch_bounds__(GW_THREADS, BF16 && MT == 1 && !ACC ? 4 : 2) void gate_narrow_kernel(GwArgs w, int blocks_w, GxArgs x, int blocks_x) {
   constexpr int V = BF16 ? 8 : 4;
   using Tile = GxTile<BF16, 1, GW_THREADS>;
   __shared__ __align__(16) unsigned char lds[Tile::LDS > GW_LDS ? Tile::LDS : GW_LDS];

@@ -986,3 +986,36 @@ def test_clip_grads_by_factors_below_the_normal_numbers():
         check_clip([t.clone() for t in g], share)
         check_clip([t.clone() for t in g], share, in_place=True)
         check_clip([t.clone() for t in g], share, out_offset=1)
+
+
+# (the last four: blocks of 64 experts)
+ALONE = [(1, 264, 24), (40, 264, 20), (64, 128, 8), (300, 520, 33), (129, 512, 65), (200, 264, 129), (257, 1024, 200),
+         (33001, 1048, 50), (40001, 1048, 64), (8200, 1048, 200), (16500, 1048, 128)]
+
+
+@pytest.mark.parametrize("T,d,E", ALONE)
+@pytest.mark.parametrize("dtype", [B.MOE_BF16, B.MOE_F32])
+def test_products_that_are_alone_in_their_sums(T, d, E, dtype):
+    """Gradients, at most one to a token and one to an expert: every row of d_w_gate and d_x is one product.  fp32 layers: eight
+    of nine piece products (the ninth is below 2^-31 of the whole), seven of them, 2^-6 of it, cut at 24 bits each, and a rounded
+    addition: 1.25 u.  d_w_gate of bf16 layers: three piece products whose sum is cut: 2.1 u.  d_x of bf16 layers: its storage."""
+    rng = np.random.default_rng([56, T, E])
+    n = min(T, E)
+    x, w = store(rng.standard_normal((T, d)), dtype), store(rng.standard_normal((E, d)), dtype)
+    t = rng.permutation(T)[:n]
+    t[:min(n, 2)] = [T - 1, 0][:min(n, 2)]
+    t = np.unique(t)
+    e = rng.permutation(E)[:t.size]
+    ds = np.zeros((T, E), dtype=np.float32)
+    ds[t, e] = rng.standard_normal(t.size) * 10.0 ** rng.integers(-6, 3, t.size)
+    sh = shape_of(T, E, 1, 0, d, dtype)
+    ws, nb = workspace(sh)
+    dw, db, dx = Guarded((E, d)), Guarded((E,)), Guarded((T, d), torch.float32 if dtype == B.MOE_F32 else torch.bfloat16)
+    B.moe_gate_backward(sh, layer.to_device(x), layer.to_device(w), dev(ds), None, dw.t, db.t, dx.t, 0, ws, nb)
+    rw, rb, rx = go.gate_backward(orc.to_f64(x), orc.to_f64(w), ds)
+    of_w, of_x = (1.25 * U, 1.25 * U) if dtype == B.MOE_F32 else (2.1 * U, 2.0 ** -8)
+    err = np.abs(dw.np() - rw)
+    assert (err <= of_w * np.abs(rw)).all(), f"d_w_gate: {(err[rw != 0] / np.abs(rw[rw != 0])).max() / U:.3f} u"
+    err = np.abs(dx.np() - rx)
+    assert (err <= of_x * np.abs(rx)).all(), f"d_x: {(err[rx != 0] / np.abs(rx[rx != 0])).max() / U:.3f} u"
+    assert np.array_equal(db.np(), rb)
