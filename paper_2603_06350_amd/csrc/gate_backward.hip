@@ -61,6 +61,12 @@ __device__ __forceinline__ void gb_split8(const float (&v)[8], uint4 (&p)[3]) {
   for (int i = 0; i < 3; ++i) p[i] = make_uint4(q[i][0], q[i][1], q[i][2], q[i][3]);
 }
 
+// The sum of a lane's eight gradients of an expert, for d_gate_bias, which is summed in 64 bits beyond these (sums in 32 were
+// off by up to 3e-7, relative, where these are by 7e-8).
+__device__ __forceinline__ float gb_sum8(const float (&v)[8]) {
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
 // The operand fragments of V column tiles from a lane's V columns of 8 rows along the reduction; P pieces each.
 template <bool BF16, int V> struct GbFrag {
   static constexpr int P = BF16 ? 1 : 3;
@@ -202,7 +208,7 @@ __device__ __forceinline__ GwPlace gw_place(int tiles, int chunks, int splits, i
 // every wave cuts the pieces of its own.
 constexpr int GW_LDS = GW_WAVES * 4 * MOE_WAVE * 16;
 template <bool BF16, int MT, int V>
-__device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, unsigned char* lds, float (*red_b)[16 * MT]) {
+__device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, unsigned char* lds, double (*red_b)[16 * MT]) {
   constexpr int B = BF16 ? 2 : 4;
   auto red = reinterpret_cast<gb_f32x4(*)[4][MOE_WAVE]>(lds);
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
@@ -218,10 +224,10 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
   const bool with_w = a.out_w, with_bias = a.out_b && tile == 0;
 
   gb_f32x4 acc[MT][V];
-  float bias[MT];
+  double bias[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    bias[m] = 0.f;
+    bias[m] = 0.0;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[m][i] = gb_f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -266,10 +272,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
     uint4 p[MT][3];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      if (with_bias) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) bias[m] += ds[m][j];
-      }
+      if (with_bias) bias[m] += gb_sum8(ds[m]);
       gb_split8(ds[m], p[m]);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -317,7 +320,7 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
   if (with_bias) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      float v = bias[m];
+      double v = bias[m];
       v += __shfl_xor(v, 16);
       v += __shfl_xor(v, 32);
       if (g == 0) red_b[wave][16 * m + c] = v;
@@ -325,9 +328,9 @@ __device__ __forceinline__ void gate_weight_block(const GwArgs& a, int block, un
     __syncthreads();
     const int e = e0 + threadIdx.x;
     if (threadIdx.x < 16 * MT && e < E) {
-      float v = add ? a.out_b[e] : 0.f;
+      double v = add ? a.out_b[e] : 0.f;
       for (int w = 0; w < GW_WAVES; ++w) v += red_b[w][threadIdx.x];
-      a.out_b[(splits > 1 ? static_cast<int64_t>(split) * E : 0) + e] = v;
+      a.out_b[(splits > 1 ? static_cast<int64_t>(split) * E : 0) + e] = static_cast<float>(v);
     }
   }
 }
@@ -348,7 +351,7 @@ constexpr int GWW_LDS = 3 * GWW_STEP;                 // (the waves' sums need 6
 static_assert(GWW_LDS >= GW_WAVES * 8 * MOE_WAVE * 16, "sums of the waves");
 
 template <bool BF16, int V>
-__device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned char* lds, float* red_b) {
+__device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned char* lds, double* red_b) {
   constexpr int B = BF16 ? 2 : 4, MT = 4;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / MOE_WAVE), c = lane & 15, g = lane >> 4;
   const int half = wave >> 2;
@@ -365,7 +368,8 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
   // this thread's part of d_scores: 8 tokens of an expert
   const uint32_t at_s = 8 * (wave & 3) * pitch_s + static_cast<uint32_t>(min(e0 + lane, E - 1)) * 4;
   const int at_piece = half * 3 * GWW_PIECES + (lane / 16 * MOE_WAVE + 16 * (wave & 3) + lane % 16) * 16;
-  float ds[8], bias = 0.f;
+  float ds[8];
+  double bias = 0.0;
   GbRow<BF16, V> x[8];
   uint32_t mask;
   auto left_of = [&](uint32_t t0) { return min(static_cast<int>(end - t0) - 32 * half, 32); };
@@ -392,10 +396,7 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
 #pragma unroll
       for (int j = 0; j < 8; ++j) ds[j] = mine >> j & 1 ? ds[j] : 0.f;
     }
-    if (with_bias) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) bias += ds[j];
-    }
+    if (with_bias) bias += gb_sum8(ds);
     uint4 p[3];
     gb_split8(ds, p);
 #pragma unroll
@@ -495,9 +496,9 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
     __syncthreads();
     const int e = e0 + threadIdx.x;
     if (threadIdx.x < 64 && e < E) {
-      float v = add ? a.out_b[e] : 0.f;
+      double v = add ? a.out_b[e] : 0.f;
       for (int w = 0; w < GW_WAVES; ++w) v += red_b[64 * w + threadIdx.x];
-      a.out_b[(splits > 1 ? static_cast<int64_t>(place.split) * E : 0) + e] = v;
+      a.out_b[(splits > 1 ? static_cast<int64_t>(place.split) * E : 0) + e] = static_cast<float>(v);
     }
   }
 }
@@ -505,7 +506,7 @@ __device__ __forceinline__ void gate_weight_wide_block(const GwArgs& a, unsigned
 template <bool BF16, int V>
 __global__ __launch_bounds__(GW_THREADS) void gate_weight_wide_kernel(GwArgs a) {
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ float red_b[GW_THREADS];
+  __shared__ double red_b[GW_THREADS];
   gate_weight_wide_block<BF16, V>(a, lds, red_b);
 }
 
@@ -515,12 +516,12 @@ __global__ __launch_bounds__(GW_THREADS) void gate_weight_wide_kernel(GwArgs a) 
 // 64 10.3 / 6.1 / 3.9; 64 of 64 x 2048 6.4 / 6.4 / 7.8; 16 of 128 x 4096 6.2 / 9.6 / 6.5.)
 constexpr int GS_THREADS = 256;
 __device__ __forceinline__ float4 gs_add(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
-__device__ __forceinline__ float gs_add(float a, float b) { return a + b; }
-template <int GROUPS, class V>
-__device__ __forceinline__ void gs_column(const V* part, V* out, int64_t n, int64_t i, int splits, int accumulate, V* lds) {
+__device__ __forceinline__ double gs_add(double a, double b) { return a + b; }
+template <int GROUPS, class S, class V>
+__device__ __forceinline__ void gs_column(const V* part, V* out, int64_t n, int64_t i, int splits, int accumulate, S* lds) {
   constexpr int COLUMNS = GS_THREADS / GROUPS;
   const int column = threadIdx.x % COLUMNS, group = threadIdx.x / COLUMNS;
-  V s{};
+  S s{};
   if (i < n) {
     for (int p = group; p < splits; p += 8 * GROUPS) {
       V v[8];
@@ -538,7 +539,8 @@ __device__ __forceinline__ void gs_column(const V* part, V* out, int64_t n, int6
   if (group == 0 && i < n) {
 #pragma unroll
     for (int u = 0; u < GROUPS - 1; ++u) s = gs_add(s, lds[u * COLUMNS + column]);
-    out[i] = accumulate ? gs_add(s, out[i]) : s;
+    if (accumulate) s = gs_add(s, out[i]);
+    out[i] = static_cast<V>(s);
   }
 }
 // Blocks: the first blocks_w for d_w_gate (n elements), the others for d_gate_bias.
@@ -550,11 +552,11 @@ __global__ __launch_bounds__(GS_THREADS) void gate_sum_kernel(const float* __res
   __shared__ float4 lds[(GROUPS - 1) * COLUMNS];
   const int column = threadIdx.x % COLUMNS, block = blockIdx.x;
   if (block < blocks_w)
-    gs_column<GROUPS>(reinterpret_cast<const float4*>(part_w), reinterpret_cast<float4*>(out_w), n / 4,
+    gs_column<GROUPS, float4>(reinterpret_cast<const float4*>(part_w), reinterpret_cast<float4*>(out_w), n / 4,
                       static_cast<int64_t>(block) * COLUMNS + column, splits, accumulate, lds);
   else
-    gs_column<GROUPS>(part_b, out_b, static_cast<int64_t>(E), static_cast<int64_t>(block - blocks_w) * COLUMNS + column, splits, accumulate,
-                      reinterpret_cast<float*>(lds));
+    gs_column<GROUPS, double>(part_b, out_b, static_cast<int64_t>(E), static_cast<int64_t>(block - blocks_w) * COLUMNS + column, splits, accumulate,
+                      reinterpret_cast<double*>(lds));
 }
 
 // ------------------------------------------------------------------------------------------------ hidden states' gradient
@@ -723,7 +725,7 @@ __global__ __launch_bounds__(GW_THREADS, BF16 && MT == 1 && !ACC ? 4 : 2) void g
   constexpr int V = BF16 ? 8 : 4;
   using Tile = GxTile<BF16, 1, GW_THREADS>;
   __shared__ __align__(16) unsigned char lds[Tile::LDS > GW_LDS ? Tile::LDS : GW_LDS];
-  __shared__ float red_b[GW_WAVES][16 * MT];
+  __shared__ double red_b[GW_WAVES][16 * MT];
   __shared__ uint32_t reals[Tile::STEP / 2];
   const int group = blockIdx.x / 8, both = min((blocks_w + 7) / 8, (blocks_x + 7) / 8);
   const bool of_w = group < 2 * both ? group % 2 == 0 : blocks_w > blocks_x;

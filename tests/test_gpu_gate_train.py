@@ -1019,3 +1019,20 @@ def test_products_that_are_alone_in_their_sums(T, d, E, dtype):
     err = np.abs(dx.np() - rx)
     assert (err <= of_x * np.abs(rx)).all(), f"d_x: {(err[rx != 0] / np.abs(rx[rx != 0])).max() / U:.3f} u"
     assert np.array_equal(db.np(), rb)
+
+
+@pytest.mark.parametrize("T,d,E", [(300, 64, 8), (70001, 64, 8), (30000, 72, 24), (5000, 64, 40), (33001, 1048, 64), (8200, 1048, 200)])
+@pytest.mark.parametrize("dtype", [B.MOE_BF16, B.MOE_F32])
+def test_bias_gradients_of_one_large_and_many_small_terms(T, d, E, dtype):
+    """Small terms below half a step of the large one: eight terms of a lane are added in 32 bits (three roundings), the rest
+    in 64, a part's sum and the whole are rounded once: 5 u of the sizes."""
+    ds = np.full((T, E), 2.0 ** -25, dtype=np.float32)
+    ds[T // 3] = 1.0
+    x = torch.zeros((T, d), dtype=torch.float32 if dtype == B.MOE_F32 else torch.bfloat16, device="cuda")
+    sh = shape_of(T, E, 1, 0, d, dtype)
+    ws, nb = workspace(sh)
+    for with_w in (True, False):
+        dw, db = Guarded((E, d)), Guarded((E,))
+        B.moe_gate_backward(sh, x, None, dev(ds), None, dw.t if with_w else None, db.t, None, 0, ws, nb)
+        ref = 1.0 + (T - 1) * 2.0 ** -25
+        assert (np.abs(db.np() - ref) <= 5 * U * ref).all(), (db.np() - ref) / U
