@@ -183,10 +183,11 @@ class GateTrainer:
         self.d_w_gate = torch.zeros((n_gates, E, d), dtype=torch.float32, **kw)
         self.d_gate_bias = torch.zeros((n_gates, E), dtype=torch.float32, **kw)
         self.grads = B.GradList([t for i in range(n_gates) for t in (self.d_w_gate[i], self.d_gate_bias[i])])
+        self.weight_grads = B.GradList([self.d_w_gate[i] for i in range(n_gates)])
         self.norm = torch.zeros((1,), dtype=torch.float32, **kw)
         # one buffer: the calls of a step follow each other on a stream
         self.ws_bytes = max(B.moe_workspace_bytes(self.shape), B.moe_train_workspace_bytes(self.shape),
-                            B.moe_grad_workspace_bytes(self.grads))
+                            B.moe_grad_workspace_bytes(self.grads), B.moe_grad_workspace_bytes(self.weight_grads))
         self.workspace = torch.empty((self.ws_bytes,), dtype=torch.uint8, **kw)
 
     def score(self, x, w_gate, scores, gate_bias=None, stream=None):
@@ -214,10 +215,11 @@ class GateTrainer:
         B.moe_gate_backward(self.shape, x, None if d_x is None else w_gate, self.d_scores, token_mask, self.d_w_gate[i],
                             self.d_gate_bias[i], d_x, B.MOE_ACCUMULATE_WEIGHTS if accumulate else 0, ws, nb, s)
 
-    def clip(self, stream=None):
-        """Scales the gradients of all gates, in place, to a norm of at most max_norm; returns `norm` (on the device)."""
+    def clip(self, stream=None, bias=True):
+        """Scales the gradients of all gates, in place, to a norm of at most max_norm; returns `norm` (on the device).
+        bias=False: of gates without a trained bias; d_gate_bias has no part in the norm and is left as it is."""
         s = torch.cuda.current_stream() if stream is None else stream
-        B.moe_clip_grads(self.grads, self.max_norm, self.norm, self.workspace, self.ws_bytes, s)
+        B.moe_clip_grads(self.grads if bias else self.weight_grads, self.max_norm, self.norm, self.workspace, self.ws_bytes, s)
         return self.norm
 
 
@@ -232,7 +234,7 @@ def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps
     w, losses = w_gate.clone(), []
     for _ in range(steps):
         trainer.enqueue(0, x_now, w, target_scores, token_mask=token_mask)
-        trainer.clip()
+        trainer.clip(bias=False)
         losses.append(trainer.loss[0].clone())
         master.grad = trainer.d_w_gate[0]
         opt.step()

@@ -1036,3 +1036,22 @@ def test_bias_gradients_of_one_large_and_many_small_terms(T, d, E, dtype):
         B.moe_gate_backward(sh, x, None, dev(ds), None, dw.t if with_w else None, db.t, None, 0, ws, nb)
         ref = 1.0 + (T - 1) * 2.0 ** -25
         assert (np.abs(db.np() - ref) <= 5 * U * ref).all(), (db.np() - ref) / U
+
+
+@pytest.mark.parametrize("max_norm", [float("inf"), 1e-3])
+def test_finetuning_clips_by_what_it_trains(max_norm):
+    """Without a trained bias the norm is that of the weights' gradient, and the bias' gradient stays unscaled."""
+    T, d, E = 200, 64, 16
+    rng = np.random.default_rng(57)
+    x, w = store(rng.standard_normal((T, d)), B.MOE_BF16), store(rng.standard_normal((E, d)) / 8, B.MOE_BF16)
+    target = (rng.standard_normal((T, E)) + 3.0 * np.arange(E) / E).astype(np.float32)      # a bias that the gate lacks
+    tr = layer.GateTrainer(T, d, E, 2, 1, B.MOE_BF16, 1, max_norm=max_norm)
+    layer.finetune_predictor(tr, layer.to_device(x), dev(target), layer.to_device(w), 1, 0.0)
+    _, g = go.gate_distill(orc.gate_scores(x, w), target)
+    dw, db, _ = go.gate_backward(orc.to_f64(x), orc.to_f64(w), g)
+    norm, (clipped,) = go.clip_grads([dw], max_norm)
+    assert float(tr.norm) == pytest.approx(norm, rel=1e-5)
+    assert np.abs(tr.d_w_gate[0].cpu().numpy() - clipped).max() <= 1e-5 * np.abs(clipped).max()
+    assert np.abs(tr.d_gate_bias[0].cpu().numpy() - db).max() <= 1e-5 * np.abs(db).max()
+    both = go.clip_grads([dw, db], max_norm)[0]
+    assert float(tr.clip()) == pytest.approx(np.hypot(min(norm, max_norm), np.linalg.norm(db)), rel=1e-5) and both > 1.01 * norm
