@@ -223,30 +223,37 @@ class GateTrainer:
         return self.norm
 
 
-def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps, lr, token_mask=None):
+def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps, lr, token_mask=None, gate_bias=None):
     """Fine-tunes the gate of `trainer` (which has one), starting from w_gate: predictor of `target_scores` from x_now.
-    Returns the new weights in w_gate's type and the losses of the steps.  The optimizer is PyTorch's Adam on an fp32 copy."""
+    gate_bias: of a gate that has one; a copy of it is trained as well.  Returns the new weights in w_gate's type, the losses
+    of the steps and, with a gate_bias, the new bias.  The optimizer is PyTorch's Adam on fp32 copies."""
     if trainer.n_gates != 1:      # clip() goes over the gradients of all gates, also those that no step here writes
         raise ValueError(f"finetune_predictor: a trainer of one gate, not of {trainer.n_gates}")
     w_gate = w_gate.detach()
     master = w_gate.float().clone().requires_grad_(True)
-    opt = torch.optim.Adam([master], lr=lr)
+    bias = None if gate_bias is None else gate_bias.detach().clone().requires_grad_(True)      # fp32: its own copy
+    opt = torch.optim.Adam([master] if bias is None else [master, bias], lr=lr)
     w, losses = w_gate.clone(), []
     for _ in range(steps):
-        trainer.enqueue(0, x_now, w, target_scores, token_mask=token_mask)
-        trainer.clip(bias=False)
+        trainer.enqueue(0, x_now, w, target_scores, gate_bias=bias, token_mask=token_mask)
+        trainer.clip(bias=bias is not None)
         losses.append(trainer.loss[0].clone())
         master.grad = trainer.d_w_gate[0]
+        if bias is not None:
+            bias.grad = trainer.d_gate_bias[0]
         opt.step()
         with torch.no_grad():
             w.copy_(master)
-    return w, [float(v) for v in losses]
+    losses = [float(v) for v in losses]
+    return (w, losses) if bias is None else (w, losses, bias.detach())
 
 
-def predicted_vs_actual_loads(pred: LoadPredictor, x_now, x_later, w_pred, gate_bias=None, stream=None, w_later=None):
-    """How well the loads predicted from the current hidden states match those the same gate (or w_later, the gate
-    that w_pred was fine-tuned to predict) sees one layer later (paper, Section 4.1 and its accuracy study): both
-    passes are the library's routing and counting; the comparison of the two small count vectors is host arithmetic.
+def predicted_vs_actual_loads(pred: LoadPredictor, x_now, x_later, w_pred, gate_bias=None, stream=None, w_later=None,
+                              bias_later=None):
+    """How well the loads predicted from the current hidden states match those the same gate (or w_later and bias_later,
+    the gate that w_pred and gate_bias were fine-tuned to predict; each is the predictor's where it is None) sees one
+    layer later (paper, Section 4.1 and its accuracy study): both passes are the library's routing and counting; the
+    comparison of the two small count vectors is host arithmetic.
     Returns (predicted counts, actual counts, fraction of (token, slot) choices that the later
     routing also makes for that token)."""
     s = torch.cuda.current_stream() if stream is None else stream
@@ -254,7 +261,8 @@ def predicted_vs_actual_loads(pred: LoadPredictor, x_now, x_later, w_pred, gate_
     with torch.cuda.stream(s):
         c_pred = pred.counts.clone()
         idx_pred = pred.topk_idx.clone()
-    pred.enqueue(x_later, w_pred if w_later is None else w_later, gate_bias, stream=s)
+    pred.enqueue(x_later, w_pred if w_later is None else w_later,
+                 gate_bias if bias_later is None else bias_later, stream=s)
     with torch.cuda.stream(s):
         same = (idx_pred.unsqueeze(2) == pred.topk_idx.unsqueeze(1)).any(dim=2).float().mean()
     s.synchronize()

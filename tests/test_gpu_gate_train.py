@@ -1055,3 +1055,33 @@ def test_finetuning_clips_by_what_it_trains(max_norm):
     assert np.abs(tr.d_gate_bias[0].cpu().numpy() - db).max() <= 1e-5 * np.abs(db).max()
     both = go.clip_grads([dw, db], max_norm)[0]
     assert float(tr.clip()) == pytest.approx(np.hypot(min(norm, max_norm), np.linalg.norm(db)), rel=1e-5) and both > 1.01 * norm
+
+
+@pytest.mark.parametrize("dtype", [B.MOE_BF16, B.MOE_F32])
+def test_finetuning_of_a_gate_with_a_bias(dtype):
+    """One step: scores and losses with the bias, a norm of both gradients, and both moved by Adam's first step, lr against
+    the gradient's sign; the bias that was given, and the later gate's, are left."""
+    T, d, E, k, lr = 200, 64, 16, 2, 1e-2
+    rng = np.random.default_rng(58)
+    x, w = store(rng.standard_normal((T, d)), dtype), store(rng.standard_normal((E, d)) / 8, dtype)
+    bias = np.linspace(-1.5, 1.5, E).astype(np.float32)
+    target = rng.standard_normal((T, E)).astype(np.float32)
+    tr = layer.GateTrainer(T, d, E, k, 1, dtype, 1, max_norm=float("inf"))
+    xd, wd, bd = layer.to_device(x), layer.to_device(w), dev(bias)
+    new, losses, new_bias = layer.finetune_predictor(tr, xd, dev(target), wd, 1, lr, gate_bias=bd)
+    loss, g = go.gate_distill(orc.gate_scores(x, w, bias), target)
+    dw, db, _ = go.gate_backward(orc.to_f64(x), orc.to_f64(w), g)
+    assert losses == [pytest.approx(loss, rel=1e-5)] and np.array_equal(bd.cpu().numpy(), bias)
+    assert float(tr.norm) == pytest.approx(go.clip_grads([dw, db], 1.0)[0], rel=1e-5)
+    moved = new_bias.double().cpu().numpy() - bias
+    assert (np.abs(moved + lr * np.sign(db))[np.abs(db) > 1e-4] <= 1e-3 * lr).all() and (np.abs(db) > 1e-4).sum() > E // 2
+    if dtype == B.MOE_F32:
+        moved, large = new.double().cpu().numpy() - orc.to_f64(w), np.abs(dw) > 1e-4
+        assert (np.abs(moved + lr * np.sign(dw))[large] <= 1e-3 * lr).all()
+    assert not new_bias.requires_grad and not new.requires_grad and new.dtype == wd.dtype
+    # the accuracy study with a bias of either gate
+    pred = layer.LoadPredictor(T, d, E, k, dtype, 1, E)
+    a = layer.predicted_vs_actual_loads(pred, xd, xd, new, new_bias, w_later=wd, bias_later=bd)
+    idx = orc.topk_select(orc.gate_scores(x, w, bias), k)
+    assert np.array_equal(a[1], np.bincount(idx.ravel(), minlength=E))
+    assert layer.predicted_vs_actual_loads(pred, xd, xd, wd, bd)[2] == 1.0
