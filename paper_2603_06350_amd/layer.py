@@ -6,6 +6,8 @@ layer so that repeated forwards allocate nothing.
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
 import torch
 
@@ -226,17 +228,18 @@ class GateTrainer:
 def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps, lr, token_mask=None, gate_bias=None):
     """Fine-tunes the gate of `trainer` (which has one), starting from w_gate: predictor of `target_scores` from x_now.
     gate_bias: of a gate that has one; a copy of it is trained as well.  Returns the new weights in w_gate's type, the losses
-    of the steps and, with a gate_bias, the new bias.  The optimizer is PyTorch's Adam on fp32 copies."""
+    of the steps and, with a gate_bias, the new bias.  The optimizer is PyTorch's Adam on fp32 copies.  ValueError if the
+    gradients of a step are not finite (an infinity or NaN in x_now or target_scores, or weights that grew out of range)."""
     if trainer.n_gates != 1:      # clip() goes over the gradients of all gates, also those that no step here writes
         raise ValueError(f"finetune_predictor: a trainer of one gate, not of {trainer.n_gates}")
     w_gate = w_gate.detach()
     master = w_gate.float().clone().requires_grad_(True)
     bias = None if gate_bias is None else gate_bias.detach().clone().requires_grad_(True)      # fp32: its own copy
     opt = torch.optim.Adam([master] if bias is None else [master, bias], lr=lr)
-    w, losses = w_gate.clone(), []
+    w, losses, norms = w_gate.clone(), [], []
     for _ in range(steps):
         trainer.enqueue(0, x_now, w, target_scores, gate_bias=bias, token_mask=token_mask)
-        trainer.clip(bias=bias is not None)
+        norms.append(trainer.clip(bias=bias is not None).clone())
         losses.append(trainer.loss[0].clone())
         master.grad = trainer.d_w_gate[0]
         if bias is not None:
@@ -245,6 +248,9 @@ def finetune_predictor(trainer: GateTrainer, x_now, target_scores, w_gate, steps
         with torch.no_grad():
             w.copy_(master)
     losses = [float(v) for v in losses]
+    for i, norm in enumerate(norms):
+        if not math.isfinite(float(norm)):
+            raise ValueError(f"finetune_predictor: the gradients of step {i} are not finite (norm {float(norm)}, loss {losses[i]})")
     return (w, losses) if bias is None else (w, losses, bias.detach())
 
 

@@ -1085,3 +1085,22 @@ def test_finetuning_of_a_gate_with_a_bias(dtype):
     idx = orc.topk_select(orc.gate_scores(x, w, bias), k)
     assert np.array_equal(a[1], np.bincount(idx.ravel(), minlength=E))
     assert layer.predicted_vs_actual_loads(pred, xd, xd, wd, bd)[2] == 1.0
+
+
+@pytest.mark.parametrize("where", ["x", "target"])
+def test_finetuning_on_what_is_not_finite_is_refused(where):
+    T, d, E = 100, 64, 8
+    gen = torch.Generator(device="cuda").manual_seed(59)
+    x, w = (torch.randn(s, generator=gen, device="cuda").bfloat16() for s in ((T, d), (E, d)))
+    target = torch.randn((T, E), generator=gen, device="cuda")
+    tr = layer.GateTrainer(T, d, E, 2, 1, B.MOE_BF16, 1)
+    mask = torch.ones(T, dtype=torch.bool, device="cuda")
+    mask[7] = False
+    if where == "x":
+        x[7, 3] = float("inf")
+    else:
+        target[7, 3] = float("nan")
+    with pytest.raises(ValueError, match="step 0"):
+        layer.finetune_predictor(tr, x, target, w, 3, 1e-3)
+    new, losses = layer.finetune_predictor(tr, x, target, w, 3, 1e-3, token_mask=mask)      # a padded token's
+    assert torch.isfinite(new.float()).all() and np.isfinite(losses).all()
