@@ -201,18 +201,20 @@ class GateTrainer:
         B.moe_route_ws(sh, x, w_gate, gate_bias, self.topk_idx, self.topk_w, scores, self.workspace, self.ws_bytes, s)
 
     def enqueue(self, i, x, w_gate, target_scores, gate_bias=None, token_mask=None, accumulate=False, d_x=None,
-                stream=None):
+                stream=None, coef=1.0):
         """Losses and gradients of gate i.  token_mask: 0 for padded tokens.  accumulate: the gradients are added to
-        those of earlier micro-batches (before clip()).  d_x: an output for the hidden states' gradient, or None."""
+        those of earlier micro-batches (before clip()).  coef: what the gradients of this call are multiplied by; micro-batches
+        add up to the gradient of the mean over all their tokens if each has its share of the tokens that count.  d_x: an
+        output for the hidden states' gradient, or None."""
         s = torch.cuda.current_stream() if stream is None else stream
         ws, nb = self.workspace, self.ws_bytes
         self.score(x, w_gate, self.scores, gate_bias, s)
-        B.moe_gate_distill(self.shape, self.scores, target_scores, token_mask, 1.0, self.loss[i:i + 1], self.d_scores, 0,
+        B.moe_gate_distill(self.shape, self.scores, target_scores, token_mask, coef, self.loss[i:i + 1], self.d_scores, 0,
                            ws, nb, s)
         B.moe_balance_loss(self.shape, self.scores, self.topk_idx, token_mask, self.counts[i], self.prob_sum,
                            self.balance[i:i + 1], ws, nb, s)
         if self.balance_coef != 0.0:
-            B.moe_route_backward(self.shape, self.scores, None, None, self.counts[i], self.balance_coef, token_mask,
+            B.moe_route_backward(self.shape, self.scores, None, None, self.counts[i], coef * self.balance_coef, token_mask,
                                  self.d_scores, 1, s)
         B.moe_gate_backward(self.shape, x, None if d_x is None else w_gate, self.d_scores, token_mask, self.d_w_gate[i],
                             self.d_gate_bias[i], d_x, B.MOE_ACCUMULATE_WEIGHTS if accumulate else 0, ws, nb, s)

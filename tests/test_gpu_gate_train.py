@@ -1104,3 +1104,28 @@ def test_finetuning_on_what_is_not_finite_is_refused(where):
         layer.finetune_predictor(tr, x, target, w, 3, 1e-3)
     new, losses = layer.finetune_predictor(tr, x, target, w, 3, 1e-3, token_mask=mask)      # a padded token's
     assert torch.isfinite(new.float()).all() and np.isfinite(losses).all()
+
+
+def test_micro_batches_add_up_to_the_mean_over_all_tokens():
+    T, d, E, k = 96, 64, 12, 2
+    rng = np.random.default_rng(60)
+    w = store(rng.standard_normal((E, d)) / 8, B.MOE_BF16)
+    tr = layer.GateTrainer(T, d, E, k, 1, B.MOE_BF16, 1, balance_coef=0.05)
+    masks = [mask_of("some", T, 61), mask_of("odd_bytes", T, 0), mask_of("one", T, 0)]
+    n = [int((m != 0).sum()) for m in masks]
+    pieces = []
+    for i, m in enumerate(masks):
+        x, target = store(rng.standard_normal((T, d)), B.MOE_BF16), rng.standard_normal((T, E)).astype(np.float32)
+        tr.enqueue(0, layer.to_device(x), layer.to_device(w), dev(target), token_mask=dev(m), accumulate=i > 0, coef=n[i] / sum(n))
+        scores, idx = orc.gate_scores(x, w), tr.topk_idx.cpu().numpy()
+        loss, _ = go.gate_distill(scores, target, 1.0, m)
+        assert float(tr.loss[0]) == pytest.approx(loss, rel=1e-5)
+        pieces.append((x, scores, target, idx, m))
+    x, scores, target, idx, m = (np.concatenate(p) for p in zip(*pieces))
+    _, g = go.gate_distill(scores, target, 1.0, m)
+    # the balance loss is each micro-batch's own, in its share
+    g = g + np.concatenate([n[i] / sum(n) * go.route_backward(s, e, None, go.balance_loss(s, e, v)[0], 0.05, 1, v, k)
+                            for i, (_, s, _, e, v) in enumerate(pieces)])
+    dw, db, _ = go.gate_backward(orc.to_f64(x), orc.to_f64(w), g, m)
+    assert np.abs(tr.d_w_gate[0].cpu().numpy() - dw).max() <= 1e-5 * np.abs(dw).max()
+    assert np.abs(tr.d_gate_bias[0].cpu().numpy() - db).max() <= 1e-5 * np.abs(dw).max()
