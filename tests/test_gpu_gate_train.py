@@ -1129,3 +1129,49 @@ def test_micro_batches_add_up_to_the_mean_over_all_tokens():
     dw, db, _ = go.gate_backward(orc.to_f64(x), orc.to_f64(w), g, m)
     assert np.abs(tr.d_w_gate[0].cpu().numpy() - dw).max() <= 1e-5 * np.abs(dw).max()
     assert np.abs(tr.d_gate_bias[0].cpu().numpy() - db).max() <= 1e-5 * np.abs(dw).max()
+
+
+@pytest.mark.parametrize("T", [32767, 32768, 32769, 40001, 65536])
+@pytest.mark.parametrize("mask", ["some", "nothing", "one", "odd_bytes", "last"])
+def test_gate_distill_of_masks_that_a_launch_counts(T, mask):
+    """From 32768 tokens on the mask is counted before the gradients are made; all of its parts have tokens."""
+    E = 8
+    rng, scores, _ = tables(T, E, 1, 62)
+    target = (scores + 0.5 * rng.standard_normal((T, E))).astype(np.float32)
+    m = mask_of(mask if mask != "last" else "nothing", T, 62)
+    if mask == "last":
+        m[[0, T // 64 - 1, T // 64, T - 1]] = 1
+    check_distill(T, E, m, scores, target, 1.0, 0)
+    check_distill(T, E, m, scores, target, -0.1 * T, 1)
+
+
+@pytest.mark.parametrize("T,d,E", [(33001, 1048, 64), (8200, 1048, 200)])
+def test_a_training_step_of_large_blocks_in_a_graph_and_on_two_streams(T, d, E):
+    """The kernels of large batches, of more than 32 experts: replayed with other inputs, and two batches at once."""
+    sh, ws, nb, _, x, w, target, mask, b = chain_setup(T, d, E, 3, 63)
+    chain(sh, ws, nb, x, w, target, mask, b, None)
+    first = snapshot(b)
+    other = chain_setup(T - 1000, d, E, 3, 64)
+    chain(*other[:3], *other[4:], None)
+    alone = snapshot(other[-1])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        chain(sh, ws, nb, x, w, target, mask, b, streams[0])
+        chain(*other[:3], *other[4:], streams[1])
+    got, got_other = snapshot(b), snapshot(other[-1])
+    assert all(torch.equal(first[n], got[n]) for n in first) and all(torch.equal(alone[n], got_other[n]) for n in alone)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(sh, ws, nb, x, w, target, mask, b, torch.cuda.current_stream())
+    for i in range(3):
+        x.copy_(torch.roll(x, 1, 0))
+        target.mul_(-1.1)
+        for n in OUTPUTS:
+            b[n].fill_(3)
+        graph.replay()
+        replayed = snapshot(b)
+        chain(sh, ws, nb, x, w, target, mask, b, None)
+        eager = snapshot(b)
+        for n in eager:
+            assert torch.equal(eager[n], replayed[n]), f"replay {i}: {n}"
