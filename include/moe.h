@@ -312,7 +312,8 @@ int moe_place_replicas(int32_t E, const int32_t* loads, const int32_t* replicas,
 
 /*
  * Training a gate.  The paper's predictors are copies of later layers' gates that are fine-tuned on stored hidden
- * states (Section 4.1); the same calls train a router.  A step is
+ * states (Section 4.1); the same calls train a router (d_topk_w then comes from the caller: the experts have no backward
+ * pass here).  A step is
  *   moe_route_ws with scores_out -> moe_gate_distill and / or moe_balance_loss + moe_route_backward
  *   -> moe_gate_backward -> moe_clip_grads over the gradients of all gates -> the caller's optimizer.
  * Common to the calls below:

@@ -6,9 +6,9 @@
 // loads, and neither hides the other entirely.
 //
 // Measured (bf16 layers; a copy on this card reads and writes 4.6 to 5.4 TB/s): both gradients of 65536 tokens, d = 4096, E = 8
-// 217 us = 5.0 TB/s; 65536 tokens, d = 2048, E = 64 111 us = 5.0 TB/s, of it the weights' 56
-// with 6.5 for the sums of the parts and the hidden states' 47 = 5.7 TB/s written; weights alone of 16384 tokens, d = 4096,
-// E = 128 50 us and 9.6.
+// 217 us = 5.0 TB/s; 65536 tokens, d = 2048, E = 64 113 to 117 us = 4.8 TB/s, of it the weights' 55
+// and 7 for the sums of the parts and the hidden states' 48 to 50 = 5.5 TB/s written; weights alone of 16384 tokens, d = 4096,
+// E = 128 50 us and 6.5.
 //
 // Both run on v_mfma_f32_16x16x32_bf16 with fp32 accumulators, operands straight from global memory into registers:
 //   - a lane that holds V consecutive columns of 8 consecutive rows of a matrix (one load per row) turns them, with
@@ -96,8 +96,8 @@ typedef uint32_t gb_u32x2 __attribute__((ext_vector_type(2)));
 
 // What is not used again by the launch (d_x as it is stored, x of large batches) is marked as a stream, so that it leaves the
 // caches first: d_x displaces less of the x that follows, and x nothing.  (Measured for both gradients, neither / stores /
-// stores and the loads of blocks of 64 experts, us: 65536 tokens, d = 2048, E = 64 145 / 126 / 114; 16384, d = 4096, E = 128
-// 110 / 109 / 96; 30000, d = 4096, E = 16 109 / 104; 8192, d = 2048, E = 64 29.4 / 29.9.  In the blocks of 16 and 32 experts
+// stores and the loads of blocks of 64 experts, us: 65536 tokens, d = 2048, E = 64 152 / 129 / 117; 16384, d = 4096, E = 128
+// 115 / 109 / 108; 30000, d = 4096, E = 16 109 / 104; 8192, d = 2048, E = 64 30.9 / 31.8.  In the blocks of 16 and 32 experts
 // marked loads are slower: 4096 tokens, d = 4096, E = 8 18.3 / 20.4 with them.)
 constexpr int GB_STREAM = 2;
 
@@ -794,8 +794,8 @@ static GxArgs gx_plan(GxArgs a, int cols, int step, int most_blocks) {
   return a;
 }
 
-// (Measured for both gradients, 256 / 512 / 1024 blocks, us: 3000 tokens, d = 4096, E = 200 50.3 / 46.9 / 49.8; 4000, d = 5120,
-// E = 100 57 / 48 / 49; 30000, d = 2048, E = 32 62.8 / 62.8 / 65.0; 65536, d = 2048, E = 64 108.6 / 111.5 / 112.)
+// (Measured for both gradients, 256 / 512 / 1024 blocks, us: 3000 tokens, d = 4096, E = 200 56 / 52 / 55; 4000, d = 5120,
+// E = 100 61 / 52 / 52; 30000, d = 2048, E = 32 62 / 65 / 68; 65536, d = 2048, E = 64 116 to 123 / 117 / 115.)
 template <bool BF16, int KS> static void launch_x(GxArgs x, bool accumulate, hipStream_t st) {
   constexpr int V = KS <= 2 ? (BF16 ? 8 : 4) : (BF16 ? 4 : 2);
   x = gx_plan(x, 16 * V * GX_SIDE, GxTile<BF16, KS, 256>::STEP, 512);
@@ -806,9 +806,9 @@ template <bool BF16, int KS> static void launch_x(GxArgs x, bool accumulate, hip
 }
 
 // One launch for both gradients, but two for 17 to 32 experts beyond a round of blocks: their weights' blocks have a CU to
-// themselves, which costs the hidden states' more than the launch.  (Measured, one launch / two, us: E = 8, d = 4096, 501
-// tokens 14.0 / 16.5, 4096 18.8 / 19.3, 65536 234 / 238; E = 32, 2000 tokens, d = 2048 14.2 / 17.0; E = 24, 32768 tokens,
-// d = 4096 145 / 136.)
+// themselves, which costs the hidden states' more than the launch.  (Measured in a captured graph, one launch / two, us: E = 8,
+// d = 4096, 501 tokens 6.4 / 9.7, 4096 19.0 / 20.2, 65536 217 / 195; E = 16, 30000 tokens 104 / 97; E = 32, 2000 tokens,
+// d = 2048 10.7 / 14.5; E = 24, 32768 tokens, d = 4096 139 / 118.  So up to 16 experts, too, large batches would gain from two.)
 template <bool BF16, int MT> static void launch_narrow(const GwArgs& w, const GxArgs& gx, bool with_w, bool with_x, bool accumulate, hipStream_t st) {
   const GxArgs x = gx_plan(gx, 16 * (BF16 ? 8 : 4) * GX_SIDE, GxTile<BF16, 1, GW_THREADS>::STEP, 512);
   const int blocks_w = with_w ? w.tiles * w.chunks * w.splits : 0;

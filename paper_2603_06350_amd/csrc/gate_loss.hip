@@ -3,10 +3,10 @@
 //                       L = E k sum_e c_e P_e / (sum c)^2
 //   moe_route_backward  the gradient of the routing weights and of coef * L
 //   moe_gate_distill    the mean over tokens of KL(softmax(target) || p), and its gradient
-// All three stream tables of T x E floats once: HBM-bound for large batches, launch-bound for small ones.  (Measured, in a
-// queue that is kept full, 65536 tokens: distill with a gradient, 128 experts, 100 MB, 22.8 us, of it 4 for the sum of the
-// loss, and 26.8 with a mask; balance and its gradient, 64 experts, 52 MB, 18.4 us in three launches; route backward, 128
-// experts, k = 8, 71 MB, 15.8 us = 4.5 TB/s.  A single small call takes 4 to 6 us.)
+// All three stream tables of T x E floats once: HBM-bound for large batches, launch-bound for small ones.  (Measured, in
+// a captured graph, 65536 tokens: distill with a gradient, 128 experts, 100 MB, 23.8 us, of it 4 for the sum of the loss,
+// and 28 with a mask; balance and its gradient, 64 experts, 52 MB, 19.4 us in three launches; route backward, 128
+// experts, k = 8, 71 MB, 16.2 us = 4.4 TB/s.  A single small call takes 4 to 6 us.)
 //
 // G lanes share a token, the least power of two with 4 G >= E; a lane holds four scores: consecutive ones in one load if
 // E is a multiple of 4 (VEC), those of experts l, l + G, ... otherwise.  So a wave reads 64 / G neighbouring rows at a
