@@ -12,12 +12,13 @@ import numpy as np
 
 
 def softmax(scores):
-    """Rows of probabilities in fp64; -inf is an expert that is switched off, and a row of nothing else is all zeros."""
+    """Rows of probabilities in fp64; -inf is an expert that is switched off, and a row of nothing else is all zeros.  A NaN
+    makes its row NaN."""
     s = np.asarray(scores, dtype=np.float64)
     m = s.max(axis=1, keepdims=True)
     e = np.exp(s - np.where(np.isneginf(m), 0.0, m))
     total = e.sum(axis=1, keepdims=True)
-    return e / np.where(total > 0.0, total, 1.0)
+    return e / np.where(total == 0.0, 1.0, total)
 
 
 def _real(token_mask, T):
@@ -92,13 +93,13 @@ def gate_distill(scores, target_scores, coef=1.0, token_mask=None):
     if rows.size == 0:
         return 0.0, grad
     p, q = softmax(scores[rows]), softmax(target_scores[rows])
-    left = (p.sum(axis=1) > 0) & (q.sum(axis=1) > 0)
+    left = (p.sum(axis=1) != 0) & (q.sum(axis=1) != 0)
     loss = 0.0
     for i in np.flatnonzero(left):
         s, t = np.asarray(scores[rows[i]], dtype=np.float64), np.asarray(target_scores[rows[i]], dtype=np.float64)
         log_p = s - s.max() - np.log(np.exp(s - s.max()).sum())
         log_q = t - t.max() - np.log(np.exp(t - t.max()).sum())
-        on = q[i] > 0
+        on = q[i] != 0
         loss += float((q[i][on] * (log_q[on] - log_p[on])).sum())
     grad[rows[left]] = coef / rows.size * (p[left] - q[left])
     return loss / rows.size, grad

@@ -145,3 +145,15 @@ def test_planted_mistakes_are_seen():
     loss, _ = go.gate_distill(scores, target, 1.0, mask)
     assert loss == pytest.approx(go.gate_distill(scores[:2], target[:2])[0], rel=1e-14)
     assert abs(loss * mask.sum() / T - loss) > 1e-3
+
+
+def test_nan_scores_are_seen():
+    rng = np.random.default_rng(6)
+    for table in (0, 1):
+        for row in ([np.nan] * 4, [0.3, np.nan, 1.0, -2.0], [-np.inf, np.nan, -np.inf, -np.inf]):
+            tables = [rng.standard_normal((3, 4)) for _ in range(2)]
+            tables[table][1] = row
+            loss, grad = go.gate_distill(*tables)
+            assert math.isnan(loss) and np.isnan(grad[1]).all() and np.isfinite(grad[[0, 2]]).all()
+            assert np.isfinite(go.gate_distill(*tables, 1.0, np.array([1, 0, 1]))[0])
+    assert np.isnan(go.balance_loss(np.array([[np.nan, 1.0]]), np.zeros((1, 1), dtype=np.int32))[1]).all()
